@@ -384,6 +384,89 @@ int deeppcr_seq_backward(const float* W, const float* bias, const float* z0, con
                          int layer, float alpha, int launch_per_layer, void* stream);
 
 /*
+ * Operators of recurrent language models.  Their sequences [B, L, w] hold one
+ * of the DEEPPCR_F32 / _BF16 / _F16 types, `dtype`, whose elements the
+ * kernels widen to float32 on reading and round (to nearest, ties to even)
+ * once on writing; states, statistics, weights and weight gradients are
+ * float32.  Where a sequence has a row stride (ld.., in elements, at least
+ * w), its row (b, l) starts at element (b L + l) ld.., and it may start at any
+ * element, so that it can be a slice of a wider projection's output or a row
+ * of a sequence; the others are contiguous.  The conventions above hold for
+ * the rest: 16-byte boundaries elsewhere, no allocation,
+ * validation before any HIP call, no wait for the GPU, no overlap of an
+ * output with another argument but where the text allows it, results that
+ * are the same run to run.  Every launch is a kernel, so that each call can
+ * sit in a captured graph.
+ */
+enum { DEEPPCR_F32 = 0, DEEPPCR_BF16 = 1, DEEPPCR_F16 = 2 };
+enum {
+    DEEPPCR_GATE_DIRECT = 0,   /* scan: a is the multiplier itself               */
+    DEEPPCR_GATE_SIGMOID = 1   /* sigmoid of the gate's argument                 */
+};
+
+/*
+ * Gated linear recurrence over the rows of B sequences, channel by channel:
+ * the system of pcr_solve_block_bidiag with diagonal blocks and a given start.
+ *   DEEPPCR_GATE_DIRECT:   x[b,l] = a[b,l] * x[b,l-1] + u[b,l]
+ *   DEEPPCR_GATE_SIGMOID:  x[b,l] = s * x[b,l-1] + (1 - s) * u[b,l],
+ *                          s = sigmoid(a[b,l])
+ * with x[b,-1] = x0[b].
+ *   a, u    [B, L, w] of type dtype, row strides lda, ldu
+ *   x0      [B, w] float32, or NULL: zero
+ *   lengths [B] int32 on the device, or NULL: sequence b has its first
+ *           lengths[b] rows (taken as 0 below 0, as L above L); what its
+ *           other rows of a and u hold does not matter (NaN included)
+ *   x       [B, L, w] of type dtype, output; rows from lengths[b] on are zero
+ *   x_last  [B, w] float32, output, or NULL: the state after row
+ *           lengths[b] - 1 (x0 for an empty sequence), not rounded to dtype;
+ *           may be x0
+ * The state is float32 throughout; x is its rounding.  Long sequences are cut
+ * into chunks of rows that are solved at once from the products of their
+ * multipliers, so a direct gate's products over consecutive rows have to stay
+ * inside the float32 range (those of multipliers in [-1, 1] do; an underflow
+ * to zero is one of theirs).
+ * workspace_bytes >= deeppcr_gated_scan_workspace_bytes(B, L, w), which is 0
+ * for invalid sizes.
+ */
+size_t deeppcr_gated_scan_workspace_bytes(int B, int L, int w);
+int deeppcr_gated_scan_forward(const void* a, long long lda, const void* u, long long ldu,
+                               const float* x0, const int* lengths, void* x, float* x_last,
+                               int B, int L, int w, int gate, int dtype, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/*
+ * Its backward pass, the transposed system: for Loss with g = dLoss/dx and
+ * g_last = dLoss/dx_last, lam[b,l] = g[b,l] + s[b,l+1] lam[b,l+1] (s the
+ * multiplier; g_last enters at row lengths[b] - 1), and
+ *   direct:   da = lam x[l-1],                    du = lam
+ *   sigmoid:  da = lam (x[l-1] - u) s (1 - s),    du = lam (1 - s)
+ *   dx0 = s[0] lam[0]  (g_last for an empty sequence)
+ *   a, u, lda, ldu, x0, lengths  as in the forward pass (u may be NULL for
+ *                 the direct gate)
+ *   x [B, L, w]   the forward pass's output; g [B, L, w] of type dtype, row
+ *                 stride ldg
+ *   g_last        [B, w] float32, or NULL: zero
+ *   da, du        [B, L, w] of type dtype, outputs; zero from row lengths[b] on
+ *   dx0           [B, w] float32, output, or NULL; may be g_last
+ * Workspace as for the forward pass.
+ */
+int deeppcr_gated_scan_backward(const void* a, long long lda, const void* u, long long ldu,
+                                const void* x, const float* x0, const int* lengths,
+                                const void* g, long long ldg, const float* g_last, void* da,
+                                void* du, float* dx0, int B, int L, int w, int gate, int dtype,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * One row of it for each of B running sequences: state_out = the recurrence
+ * applied to state (float32, [B, w]), x = state_out rounded to dtype.
+ *   a, u [B, w] of type dtype, row strides lda, ldu; x [B, w], or NULL
+ *   state_out may be state (a running state advances in place)
+ */
+int deeppcr_gated_scan_step(const void* a, long long lda, const void* u, long long ldu,
+                            const float* state, float* state_out, void* x, int B, int w,
+                            int gate, int dtype, void* stream);
+
+/*
  * Instrumentation (not part of the numerical path).  While enabled, the
  * library brackets its kernel launches with HIP events on the launch's own
  * stream and records, per kernel class, the launch count, the summed device
@@ -403,7 +486,8 @@ enum {
     DEEPPCR_KCLASS_OTHER = 4,      /* initial guess, copies, dz0               */
     DEEPPCR_KCLASS_SEQUENTIAL = 5, /* sequential baseline passes               */
     DEEPPCR_KCLASS_PCR_TAIL = 6,   /* substitution inside chunks, or row by row */
-    DEEPPCR_KCLASS_COUNT = 7
+    DEEPPCR_KCLASS_SCAN = 7,       /* gated scan                               */
+    DEEPPCR_KCLASS_COUNT = 8
 };
 int deeppcr_profile_enable(int on);
 /* Times only the classes whose bit (1 << class) is set in `class_mask` (all

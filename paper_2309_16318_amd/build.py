@@ -16,7 +16,8 @@ OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libdeeppcr.so")
 
 SOURCES = ["api.hip", "layers.hip", "tiny.hip", "sequential.hip", "small.hip",
-           "resnet.hip", "chunked.hip", "wide.hip", "panels.hip", "blocks.hip"]
+           "resnet.hip", "chunked.hip", "wide.hip", "panels.hip", "blocks.hip",
+           "scan.hip"]
 ARCH = "gfx950"
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",

@@ -1485,6 +1485,173 @@ int deeppcr_seq_backward(const float* W, const float* bias, const float* z0, con
     return DEEPPCR_OK;
 }
 
+// ------------------------------------------------ recurrent language models
+}  // extern "C"
+
+namespace {
+
+int elem_size(int dtype) { return dtype == DEEPPCR_F32 ? 4 : 2; }
+
+// A launch has fewer than 2^32 threads, so the channels of a batch are limited.
+bool seq_ok(int B, int L, int w, int dtype) {
+    return B >= 1 && L >= 1 && w >= 1 && dtype >= DEEPPCR_F32 && dtype <= DEEPPCR_F16 &&
+           (double)B * w < 2147483648.0 && (double)B * L * w * 4.0 < 9.0e18;
+}
+
+// A sequence with a row stride starts at any element.
+bool on_element(std::initializer_list<const void*> ps, int e) {
+    for (const void* p : ps)
+        if ((uintptr_t)p % e != 0) return false;
+    return true;
+}
+
+// An argument's memory: n rows of w elements of e bytes, ld apart.
+struct Extent {
+    const void* p;
+    size_t n;
+};
+Extent extent(const void* p, double rows, int w, long long ld, int e) {
+    return {p, p ? ((size_t)(rows - 1) * (size_t)ld + (size_t)w) * (size_t)e : 0};
+}
+bool stride_ok(double rows, int w, long long ld, int e) {
+    return ld >= w && rows * (double)ld * e < 9.0e18;
+}
+// Whether an output overlaps an input or another output; outs[i] may be
+// exactly ins[same[i]] (-1: none).
+bool clash(std::initializer_list<Extent> ins, std::initializer_list<Extent> outs,
+           std::initializer_list<const void*> same) {
+    auto s = same.begin();
+    for (auto o = outs.begin(); o != outs.end(); ++o, ++s) {
+        for (const Extent& i : ins)
+            if (overlaps(o->p, o->n, i.p, i.n) && !(*s && i.p == *s && o->p == *s)) return true;
+        for (auto q = o + 1; q != outs.end(); ++q)
+            if (overlaps(o->p, o->n, q->p, q->n)) return true;
+    }
+    return false;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t deeppcr_gated_scan_workspace_bytes(int B, int L, int w) {
+    return seq_ok(B, L, w, DEEPPCR_F32) ? scan_workspace(B, L, w) : 0;
+}
+
+int deeppcr_gated_scan_forward(const void* a, long long lda, const void* u, long long ldu,
+                               const float* x0, const int* lengths, void* x, float* x_last, int B,
+                               int L, int w, int gate, int dtype, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+    const SpanGuard span_guard;
+    if (!a || !u || !x || !workspace || !seq_ok(B, L, w, dtype)) return DEEPPCR_EINVAL;
+    if (gate != DEEPPCR_GATE_DIRECT && gate != DEEPPCR_GATE_SIGMOID) return DEEPPCR_EINVAL;
+    const int e = elem_size(dtype);
+    if (!on_element({a, u}, e) || !aligned({x0, lengths, x, x_last, workspace}))
+        return DEEPPCR_EINVAL;
+    const double rows = (double)B * L;
+    if (!stride_ok(rows, w, lda, e) || !stride_ok(rows, w, ldu, e)) return DEEPPCR_EINVAL;
+    const size_t need = scan_workspace(B, L, w), state = (size_t)B * w * 4;
+    if (workspace_bytes < need) return DEEPPCR_EWORKSPACE;
+    if (clash({extent(a, rows, w, lda, e), extent(u, rows, w, ldu, e), {x0, x0 ? state : 0},
+               {lengths, lengths ? (size_t)B * 4 : 0}},
+              {extent(x, rows, w, w, e), {x_last, x_last ? state : 0}, {workspace, need}},
+              {nullptr, x0, nullptr}))
+        return DEEPPCR_EINVAL;
+    ScanArgs k{};
+    k.a = a;
+    k.u = u;
+    k.lda = lda;
+    k.ldu = ldu;
+    k.x0 = x0;
+    k.lengths = lengths;
+    k.out0 = x;
+    k.last = x_last;
+    k.ws = workspace;
+    k.B = B;
+    k.L = L;
+    k.w = w;
+    hipStream_t st = (hipStream_t)stream;
+    const double n = rows * w;
+    const hipError_t err = timed(DEEPPCR_KCLASS_SCAN, 3.0 * n * e + 2.0 * state, 2.0 * n, st, [&] {
+        return launch_scan(false, k, gate, dtype, st);
+    });
+    return err != hipSuccess ? hip_fail(err, "gated scan") : DEEPPCR_OK;
+}
+
+int deeppcr_gated_scan_backward(const void* a, long long lda, const void* u, long long ldu,
+                                const void* x, const float* x0, const int* lengths, const void* g,
+                                long long ldg, const float* g_last, void* da, void* du, float* dx0,
+                                int B, int L, int w, int gate, int dtype, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+    const SpanGuard span_guard;
+    if (!a || !x || !g || !da || !du || !workspace || !seq_ok(B, L, w, dtype))
+        return DEEPPCR_EINVAL;
+    if (gate != DEEPPCR_GATE_DIRECT && gate != DEEPPCR_GATE_SIGMOID) return DEEPPCR_EINVAL;
+    if (gate == DEEPPCR_GATE_SIGMOID && !u) return DEEPPCR_EINVAL;
+    const int e = elem_size(dtype);
+    if (!on_element({a, u, g}, e) ||
+        !aligned({x, x0, lengths, g_last, da, du, dx0, workspace}))
+        return DEEPPCR_EINVAL;
+    const double rows = (double)B * L;
+    if (!stride_ok(rows, w, lda, e) || (u && !stride_ok(rows, w, ldu, e)) ||
+        !stride_ok(rows, w, ldg, e))
+        return DEEPPCR_EINVAL;
+    const size_t need = scan_workspace(B, L, w), state = (size_t)B * w * 4;
+    if (workspace_bytes < need) return DEEPPCR_EWORKSPACE;
+    if (clash({extent(a, rows, w, lda, e), extent(u, rows, w, ldu, e), extent(x, rows, w, w, e),
+               extent(g, rows, w, ldg, e), {x0, x0 ? state : 0}, {g_last, g_last ? state : 0},
+               {lengths, lengths ? (size_t)B * 4 : 0}},
+              {extent(da, rows, w, w, e), extent(du, rows, w, w, e), {dx0, dx0 ? state : 0},
+               {workspace, need}},
+              {nullptr, nullptr, g_last, nullptr}))
+        return DEEPPCR_EINVAL;
+    ScanArgs k{};
+    k.a = a;
+    k.u = u;
+    k.x = x;
+    k.g = g;
+    k.lda = lda;
+    k.ldu = ldu;
+    k.ldg = ldg;
+    k.x0 = x0;
+    k.g_last = g_last;
+    k.lengths = lengths;
+    k.out0 = da;
+    k.out1 = du;
+    k.last = dx0;
+    k.ws = workspace;
+    k.B = B;
+    k.L = L;
+    k.w = w;
+    hipStream_t st = (hipStream_t)stream;
+    const double n = rows * w;
+    const hipError_t err = timed(DEEPPCR_KCLASS_SCAN,
+                                 (gate == DEEPPCR_GATE_SIGMOID ? 6.0 : 5.0) * n * e + 3.0 * state,
+                                 4.0 * n, st, [&] { return launch_scan(true, k, gate, dtype, st); });
+    return err != hipSuccess ? hip_fail(err, "gated scan backward") : DEEPPCR_OK;
+}
+
+int deeppcr_gated_scan_step(const void* a, long long lda, const void* u, long long ldu,
+                            const float* state, float* state_out, void* x, int B, int w, int gate,
+                            int dtype, void* stream) {
+    const SpanGuard span_guard;
+    if (!a || !u || !state || !state_out || !seq_ok(B, 1, w, dtype)) return DEEPPCR_EINVAL;
+    if (gate != DEEPPCR_GATE_DIRECT && gate != DEEPPCR_GATE_SIGMOID) return DEEPPCR_EINVAL;
+    const int e = elem_size(dtype);
+    if (!on_element({a, u}, e) || !aligned({state, state_out, x})) return DEEPPCR_EINVAL;
+    if (!stride_ok(B, w, lda, e) || !stride_ok(B, w, ldu, e)) return DEEPPCR_EINVAL;
+    const size_t ns = (size_t)B * w * 4;
+    if (clash({extent(a, B, w, lda, e), extent(u, B, w, ldu, e), {state, ns}},
+              {{state_out, ns}, extent(x, B, w, w, e)}, {state, nullptr}))
+        return DEEPPCR_EINVAL;
+    hipStream_t st = (hipStream_t)stream;
+    const double n = (double)B * w;
+    const hipError_t err = timed(DEEPPCR_KCLASS_SCAN, n * (3.0 * e + 8.0), 2.0 * n, st, [&] {
+        return launch_scan_step(a, lda, u, ldu, state, state_out, x, B, w, gate, dtype, st);
+    });
+    return err != hipSuccess ? hip_fail(err, "gated scan step") : DEEPPCR_OK;
+}
+
 void deeppcr_release_thread_state(void) {
     (void)prof_break();
     for (auto& p : g_prof.pending) {

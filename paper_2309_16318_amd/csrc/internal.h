@@ -371,4 +371,24 @@ hipError_t launch_newton_tiny(const float* W, const float* bias, const float* z0
                               const float* Z_init, int B, int L, int w, int layer, float alpha,
                               const StopRule& rule, unsigned* result, hipStream_t stream);
 
+// ------------------------------------------------------------- gated scan
+// x_l = s_l x_{l-1} + r_l over the rows of every sequence, and backwards.
+struct ScanArgs {
+    const void *a, *u;      // [B, L, w], row strides lda, ldu
+    const void *x, *g;      // backward: the states [B, L, w]; dLoss/dx, row stride ldg
+    long long lda, ldu, ldg;
+    const float* x0;        // [B, w] or null
+    const float* g_last;    // backward: [B, w] or null
+    const int* lengths;     // [B] or null
+    void *out0, *out1;      // x; backward: da, du
+    float* last;            // x_last; backward: dx0; or null
+    void* ws;               // scan_workspace bytes
+    int B, L, w;
+};
+size_t scan_workspace(int B, int L, int w);
+hipError_t launch_scan(bool bwd, const ScanArgs& k, int gate, int dtype, hipStream_t st);
+hipError_t launch_scan_step(const void* a, long long lda, const void* u, long long ldu,
+                            const float* state, float* state_out, void* x, int B, int w, int gate,
+                            int dtype, hipStream_t st);
+
 }  // namespace deeppcr

@@ -15,9 +15,12 @@ OK, EINVAL, ENOCONV, ENONFINITE, EHIP, EWORKSPACE = range(6)
 TANH_MLP, TANH_RESIDUAL, SIGMOID_MLP, SIGMOID_RESIDUAL, RELU_MLP, RELU_RESIDUAL = range(6)
 OP_PCR, OP_FWD, OP_BWD = 0, 1, 2
 ACT_TANH, ACT_SIGMOID, ACT_RELU = 0, 1, 2
+F32, BF16, F16 = range(3)
+GATE_DIRECT, GATE_SIGMOID = 0, 1
 (KCLASS_PCR_LEVEL, KCLASS_LAYER, KCLASS_UPDATE, KCLASS_WGRAD, KCLASS_OTHER, KCLASS_SEQUENTIAL,
- KCLASS_PCR_TAIL) = range(7)
-KCLASS_NAMES = ("pcr_level", "layer", "update", "wgrad", "other", "sequential", "pcr_tail")
+ KCLASS_PCR_TAIL, KCLASS_SCAN) = range(8)
+KCLASS_NAMES = ("pcr_level", "layer", "update", "wgrad", "other", "sequential", "pcr_tail",
+                "scan")
 MAX_WIDTH = 1024
 MAX_BLOCK_WIDTH = 128  # collapsed-skip ResNet and the chunked solve
 
@@ -70,6 +73,15 @@ SIGNATURES = {
                                                                           _c.c_void_p]),
     "deeppcr_seq_backward": (_c.c_int, [_c.c_void_p] * 7 + [_c.c_int] * 4 + [_c.c_float, _c.c_int,
                                                                            _c.c_void_p]),
+    "deeppcr_gated_scan_workspace_bytes": (_c.c_size_t, [_c.c_int] * 3),
+    "deeppcr_gated_scan_forward": (_c.c_int, [_c.c_void_p, _c.c_longlong] * 2 +
+                                   [_c.c_void_p] * 4 + [_c.c_int] * 5 +
+                                   [_c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "deeppcr_gated_scan_backward": (_c.c_int, [_c.c_void_p, _c.c_longlong] * 2 +
+                                    [_c.c_void_p] * 4 + [_c.c_longlong] + [_c.c_void_p] * 4 +
+                                    [_c.c_int] * 5 + [_c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "deeppcr_gated_scan_step": (_c.c_int, [_c.c_void_p, _c.c_longlong] * 2 + [_c.c_void_p] * 3 +
+                                [_c.c_int] * 4 + [_c.c_void_p]),
     "deeppcr_profile_enable": (_c.c_int, [_c.c_int]),
     "deeppcr_profile_select": (_c.c_int, [_c.c_uint]),
     "deeppcr_profile_reset": (None, []),
@@ -463,6 +475,165 @@ def deeppcr_seq_backward(W, bias, z0, Z, G, layer: int = TANH_MLP, alpha: float 
     if st != OK:
         raise DeepPCRError(st, "deeppcr_seq_backward")
     return Lambda, dz0
+
+
+# ------------------------------------------------ recurrent language models
+def _dtype_code(t, name):
+    torch = _torch()
+    code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, not {t.dtype}")
+    return code
+
+
+def _rows(t, shape, name, like):
+    """Checks a sequence [.., w] of like's type on like's device whose rows lie
+    a fixed stride apart (a slice of a wider tensor's last axis, say);
+    returns that stride."""
+    if t.dtype != like.dtype or t.device != like.device or not t.is_cuda:
+        raise ValueError(f"{name} must be a {like.dtype} GPU tensor on {like.device}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    w = shape[-1]
+    ld, n = None, 1
+    for size, stride in zip(reversed(shape[:-1]), reversed(t.stride()[:-1])):
+        if size > 1:
+            if ld is None:
+                ld = stride
+            elif stride != ld * n:
+                raise ValueError(f"the rows of {name} must lie a fixed stride apart")
+        n *= size
+    ld = w if ld is None else ld
+    if (w > 1 and t.stride(-1) != 1) or ld < w:
+        raise ValueError(f"the rows of {name} must be contiguous and apart")
+    return ld
+
+
+def _typed(t, shape, name, dtype, device):
+    """Checks a contiguous tensor of the given type; None passes."""
+    if t is None:
+        return
+    if t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor on {device}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+
+
+def _launch(name, stream, device, args, made):
+    """Calls entry point `name` with `args` and the stream, on `device`; what
+    the binding allocated (`made`) stays allocated until the stream is past it."""
+    torch = _torch()
+    with torch.cuda.device(device):
+        s = torch.cuda.current_stream(device) if stream is None else stream
+        st = getattr(lib(), name)(*args, ctypes.c_void_p(s.cuda_stream))
+        if stream is not None:
+            for t in made:
+                if t is not None:
+                    t.record_stream(stream)
+    if st != OK:
+        raise DeepPCRError(st, name)
+
+
+def _space(workspace, nbytes, device, made):
+    torch = _torch()
+    if workspace is None:
+        workspace = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
+        made.append(workspace)
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {device}")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def gated_scan_workspace_bytes(B: int, L: int, w: int) -> int:
+    return int(lib().deeppcr_gated_scan_workspace_bytes(B, L, w))
+
+
+def deeppcr_gated_scan_forward(a, u, x0=None, lengths=None, gate: int = GATE_DIRECT, x=None,
+                               x_last=None, workspace=None, stream=None):
+    """x_l = s_l x_{l-1} + r_l over [B, L, w] (direct: s = a, r = u; sigmoid:
+    s = sigmoid(a), r = (1 - s) u) from x0; returns (x, x_last)."""
+    torch = _torch()
+    dt = _dtype_code(a, "a")
+    B, L, w = a.shape
+    dev = a.device
+    lda, ldu = _rows(a, (B, L, w), "a", a), _rows(u, (B, L, w), "u", a)
+    _typed(x0, (B, w), "x0", torch.float32, dev)
+    _typed(lengths, (B,), "lengths", torch.int32, dev)
+    made = []
+    if x is None:
+        x = torch.empty((B, L, w), dtype=a.dtype, device=dev)
+        made.append(x)
+    if x_last is None:
+        x_last = torch.empty((B, w), dtype=torch.float32, device=dev)
+        made.append(x_last)
+    _typed(x, (B, L, w), "x", a.dtype, dev)
+    _typed(x_last, (B, w), "x_last", torch.float32, dev)
+    ws, nbytes = _space(workspace, gated_scan_workspace_bytes(B, L, w), dev, made)
+    _launch("deeppcr_gated_scan_forward", stream, dev,
+            (_ptr(a), lda, _ptr(u), ldu, _ptr(x0), _ptr(lengths), _ptr(x), _ptr(x_last), B, L, w,
+             int(gate), dt, _ptr(ws), nbytes), made)
+    return x, x_last
+
+
+def deeppcr_gated_scan_backward(a, u, x, g, g_last=None, x0=None, lengths=None,
+                                gate: int = GATE_DIRECT, da=None, du=None, dx0=None,
+                                workspace=None, stream=None):
+    """Backward pass of the gated scan from its output x, for g = dLoss/dx and
+    g_last = dLoss/dx_last; returns (da, du, dx0).  u may be None for the
+    direct gate."""
+    torch = _torch()
+    dt = _dtype_code(a, "a")
+    B, L, w = a.shape
+    dev = a.device
+    lda, ldg = _rows(a, (B, L, w), "a", a), _rows(g, (B, L, w), "g", a)
+    ldu = 0 if u is None else _rows(u, (B, L, w), "u", a)
+    _typed(x, (B, L, w), "x", a.dtype, dev)
+    for t, n in ((x0, "x0"), (g_last, "g_last")):
+        _typed(t, (B, w), n, torch.float32, dev)
+    _typed(lengths, (B,), "lengths", torch.int32, dev)
+    made = []
+    if da is None:
+        da = torch.empty((B, L, w), dtype=a.dtype, device=dev)
+        made.append(da)
+    if du is None:
+        du = torch.empty((B, L, w), dtype=a.dtype, device=dev)
+        made.append(du)
+    if dx0 is None:
+        dx0 = torch.empty((B, w), dtype=torch.float32, device=dev)
+        made.append(dx0)
+    for t, n in ((da, "da"), (du, "du")):
+        _typed(t, (B, L, w), n, a.dtype, dev)
+    _typed(dx0, (B, w), "dx0", torch.float32, dev)
+    ws, nbytes = _space(workspace, gated_scan_workspace_bytes(B, L, w), dev, made)
+    _launch("deeppcr_gated_scan_backward", stream, dev,
+            (_ptr(a), lda, _ptr(u), ldu, _ptr(x), _ptr(x0), _ptr(lengths), _ptr(g), ldg,
+             _ptr(g_last), _ptr(da), _ptr(du), _ptr(dx0), B, L, w, int(gate), dt, _ptr(ws),
+             nbytes), made)
+    return da, du, dx0
+
+
+def deeppcr_gated_scan_step(a, u, state, gate: int = GATE_DIRECT, x=None, state_out=None,
+                            stream=None):
+    """One row [B, w] of the gated scan on running float32 states; writes the
+    new states to state_out (default: state, in place) and returns x, the
+    states in a's type."""
+    torch = _torch()
+    dt = _dtype_code(a, "a")
+    B, w = a.shape
+    dev = a.device
+    lda, ldu = _rows(a, (B, w), "a", a), _rows(u, (B, w), "u", a)
+    made = []
+    if x is None:
+        x = torch.empty((B, w), dtype=a.dtype, device=dev)
+        made.append(x)
+    state_out = state if state_out is None else state_out
+    _typed(state, (B, w), "state", torch.float32, dev)
+    _typed(state_out, (B, w), "state_out", torch.float32, dev)
+    _typed(x, (B, w), "x", a.dtype, dev)
+    _launch("deeppcr_gated_scan_step", stream, dev,
+            (_ptr(a), lda, _ptr(u), ldu, _ptr(state), _ptr(state_out), _ptr(x), B, w, int(gate),
+             dt), made)
+    return x
 
 
 def release_thread_state() -> None:

@@ -1,0 +1,280 @@
+"""Gated scan on the GPU against its float64 definition: types, gates, odd
+sizes, chunk ends, padded batches, strides, streams and captured graphs.
+
+Bounds.  A row's update s x + r errs by a few float32 roundings (2^-24 of each
+term: the fused multiply-add, and the gate's exponential, reciprocal and
+product, at most 8 together), and so does each factor of a product that carries
+a state over a chunk; the errors run on through the recurrence itself, so the
+error of a state is at most the recurrence of |s| applied to 10 * 2^-24 times
+the terms' sizes.  An output's rounding adds half a step of its type.  A
+sigmoid below float32's smallest normal number 2^-126 (a logit beyond -87.3) is
+zero, because the hardware's exponential has no subnormal results: it is off by
+at most 2^-126, its products by that times the other factors.
+"""
+import numpy as np
+import pytest
+
+from oracle import scan_oracle as so
+from paper_2309_16318_amd import deeppcr
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+E32 = 2.0 ** -24
+TINY = 2.0 ** -126
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+SIZES = [(1, 1, 1), (1, 2, 64), (2, 3, 5), (3, 16, 64), (2, 17, 8), (1, 127, 2), (2, 128, 130),
+         (1, 129, 96), (4, 255, 66), (5, 256, 16), (1, 257, 33), (7, 500, 100), (64, 40, 12),
+         (2, 2049, 24), (1, 4100, 129), (300, 9, 7)]
+
+
+@pytest.fixture(scope="module")
+def dev():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return torch.device("cuda:0")
+
+
+def cpu(t):
+    return t.detach().double().cpu().numpy()
+
+
+def bound_of(s, terms):
+    """The recurrence of |s| on 10 * 2^-24 terms: how far a state may be off."""
+    e = np.zeros_like(terms)
+    run = np.zeros(terms[:, 0].shape)
+    for l in range(terms.shape[1]):
+        run = np.abs(s[:, l]) * run + 10 * E32 * terms[:, l]
+        e[:, l] = run
+    return e
+
+
+def check(got, ref, bound, dtype, what):
+    got, half = cpu(got), torch.finfo(dtype).eps / 2
+    tiny = torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+    assert got.shape == ref.shape
+    lim = bound * (1 + half) + half * np.abs(ref) + tiny
+    assert np.all(np.isfinite(got)), what
+    worst = np.max(np.abs(got - ref) - lim, initial=-np.inf)
+    assert worst <= 0, (what, worst, np.unravel_index(np.argmax(np.abs(got - ref) - lim), ref.shape))
+
+
+def inputs(B, L, w, gate, dtype, dev, seed=0, strided=False):
+    gen = torch.Generator().manual_seed(seed + 31 * B + 7 * L + w)
+    r = lambda *s: torch.randn(*s, generator=gen)
+    a = 1.5 + 1.5 * r(B, L, w) if gate == so.SIGMOID else \
+        1.0 - 1.2 * torch.rand(B, L, w, generator=gen)
+    u, g = r(B, L, w), r(B, L, w)
+    if strided:
+        wide = torch.cat([a, u, g, r(B, L, 8)], dim=2).to(dtype).to(dev)
+        a, u, g = wide[..., :w], wide[..., w:2 * w], wide[..., 2 * w:3 * w]
+    else:
+        a, u, g = (t.to(dtype).to(dev) for t in (a, u, g))
+    return a, u, g, r(B, w).to(dev), r(B, w).to(dev)
+
+
+def both(a, u, g, x0, g_last, lengths, gate, dtype, what=""):
+    """Runs and checks forward and backward; the backward on the stored states."""
+    ln = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device=a.device)
+    x, last = deeppcr.deeppcr_gated_scan_forward(a, u, x0=x0, lengths=ln, gate=gate)
+    da, du, dx0 = deeppcr.deeppcr_gated_scan_backward(a, u, x, g, g_last=g_last, x0=x0,
+                                                      lengths=ln, gate=gate)
+    torch.cuda.synchronize()
+    A, U, G, X0, GL = (None if t is None else cpu(t) for t in (a, u, g, x0, g_last))
+    B, L, w = A.shape
+    n = so.clamp_lengths(lengths, B, L)
+    there = (np.arange(L)[None, :] < n[:, None])[..., None]
+    A, U, G = (np.where(there, t, 0.0) for t in (A, U, G))
+    rx, rlast = so.scan_forward(A, U, X0, lengths, gate)
+    s, q = so.gates(A, gate)
+    first = np.zeros((B, 1, w)) if X0 is None else X0[:, None]
+    before = np.concatenate([first, rx[:, :-1]], axis=1)
+    s = np.where(there, s, 1.0)
+    ex = bound_of(s, there * (np.abs(s * before) + np.abs(q * U)
+                              + TINY / E32 * (np.abs(before) + np.abs(U))))
+    check(x, rx, ex * there, dtype, what + " x")
+    check(last, rlast, ex[:, -1], torch.float32, what + " x_last")
+    X = cpu(x)
+    rda, rdu, rdx0, lam = so.scan_backward(A, U, X, G, GL, X0, lengths, gate)
+    gl = np.zeros((B, w)) if GL is None else GL
+    after = np.concatenate([s[:, 1:], np.ones((B, 1, w))], axis=1)
+    # terms of the adjoint's update: g and what comes from the rows behind
+    ahead = np.concatenate([(s * lam)[:, 1:], gl[:, None]], axis=1)
+    el = bound_of(after[:, ::-1], (there * (np.abs(G) + np.abs(ahead)))[:, ::-1])[:, ::-1]
+    el = el + 2 * E32 * np.abs(lam)
+    sub = TINY * np.abs(lam)
+    xp = np.concatenate([first, X[:, :-1]], axis=1)
+    fac = np.abs(xp - U) * s * q if gate == so.SIGMOID else np.abs(xp)
+    mag = (np.abs(xp) + np.abs(U)) * s * q if gate == so.SIGMOID else np.abs(xp)
+    check(da, rda, there * (el * fac + 10 * E32 * np.abs(lam) * mag
+                            + sub * (np.abs(xp) + np.abs(U))), dtype, what + " da")
+    check(du, rdu, there * (el * q + 10 * E32 * np.abs(lam) * q + sub), dtype, what + " du")
+    check(dx0, rdx0, np.abs(s[:, 0]) * el[:, 0] + 10 * E32 * np.abs(s[:, 0] * lam[:, 0])
+          + sub[:, 0], torch.float32, what + " dx0")
+    return x, last, da, du, dx0
+
+
+@pytest.mark.parametrize("size", SIZES, ids=str)
+@pytest.mark.parametrize("gate", [so.DIRECT, so.SIGMOID])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_sizes(dev, size, gate, kind):
+    t = inputs(*size, gate, TYPES[kind], dev)
+    both(*t, None, gate, TYPES[kind])
+
+
+@pytest.mark.parametrize("gate", [so.DIRECT, so.SIGMOID])
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("L", [5, 130, 1100])
+def test_padded_batches(dev, gate, kind, L):
+    """Empty, full, negative and too long; NaN behind the ends does no harm,
+    and the rows there are written as zero."""
+    lengths = [L, 0, 1, L - 1, -3, L + 9, L // 2]
+    a, u, g, x0, gl = inputs(len(lengths), L, 20, gate, TYPES[kind], dev)
+    n = so.clamp_lengths(lengths, len(lengths), L)
+    for b, k in enumerate(n):
+        for t in (a, u, g):
+            t[b, k:] = float("nan")
+    x, last, da, du, dx0 = both(a, u, g, x0, gl, lengths, gate, TYPES[kind])
+    for b, k in enumerate(n):
+        for t in (x, da, du):
+            assert torch.all(t[b, k:] == 0)
+        if k == 0:
+            assert torch.equal(last[b], x0[b]) and torch.equal(dx0[b], gl[b])
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("size", [(2, 300, 48), (3, 70, 8), (1, 9, 40)], ids=str)
+def test_slices_of_a_projection(dev, kind, size):
+    for gate in (so.DIRECT, so.SIGMOID):
+        t = inputs(*size, gate, TYPES[kind], dev, strided=True)
+        assert t[0].stride(1) == 3 * size[2] + 8
+        both(*t, None, gate, TYPES[kind])
+
+
+def test_no_start_and_no_last_gradient(dev):
+    a, u, g, _, _ = inputs(2, 600, 40, so.SIGMOID, torch.bfloat16, dev)
+    both(a, u, g, None, None, None, so.SIGMOID, torch.bfloat16)
+
+
+def test_long_sequences(dev):
+    """Many chunks, gates near one: the state's errors add up over the rows."""
+    for gate in (so.DIRECT, so.SIGMOID):
+        a, u, g, x0, gl = inputs(1, 33000, 6, gate, torch.float32, dev)
+        a = (1 - 1e-3 * torch.rand_like(a)) if gate == so.DIRECT else a + 5
+        both(a, u, g, x0, gl, None, gate, torch.float32)
+
+
+def test_saturated_gates(dev):
+    """Logits of +-100 and beyond exp's range, multipliers 0, 1 and -1."""
+    a, u, g, x0, gl = inputs(2, 300, 64, so.SIGMOID, torch.float32, dev)
+    a = torch.where(torch.rand_like(a) < 0.5, 100.0, -100.0)
+    a[:, ::7] = 1e4
+    a[:, 3::7] = -1e4
+    both(a, u, g, x0, gl, None, so.SIGMOID, torch.float32)
+    a = torch.randint(-1, 2, a.shape, device=dev).float()
+    both(a, u, g, x0, gl, None, so.DIRECT, torch.float32)
+
+
+def test_growing_products_on_an_empty_state(dev):
+    """Multipliers of 1.2 over a chunk and more, inputs that stay in range."""
+    a, u, g, x0, gl = inputs(1, 300, 8, so.DIRECT, torch.float32, dev)
+    a = torch.full_like(a, 1.2)
+    both(a, u * 1e-10, g * 1e-10, x0 * 0, gl * 0, None, so.DIRECT, torch.float32)
+
+
+def test_a_nan_stays_in_its_channel_and_behind_its_row(dev):
+    a, u, g, x0, gl = inputs(2, 700, 40, so.SIGMOID, torch.bfloat16, dev)
+    clean = deeppcr.deeppcr_gated_scan_forward(a, u, x0=x0, gate=so.SIGMOID)[0]
+    u[1, 333, 17] = float("nan")
+    x = deeppcr.deeppcr_gated_scan_forward(a, u, x0=x0, gate=so.SIGMOID)[0]
+    bad = torch.zeros_like(x, dtype=torch.bool)
+    bad[1, 333:, 17] = True
+    assert torch.equal(torch.isnan(x), bad)
+    assert torch.equal(x[~bad], clean[~bad])
+
+
+def test_states_in_place(dev):
+    """x_last over x0 and dx0 over g_last, at one chunk and at many."""
+    for L in (3, 100, 1000):
+        a, u, g, x0, gl = inputs(3, L, 72, so.SIGMOID, torch.bfloat16, dev)
+        x, last = deeppcr.deeppcr_gated_scan_forward(a, u, x0=x0, gate=so.SIGMOID)
+        _, _, dx0 = deeppcr.deeppcr_gated_scan_backward(a, u, x, g, g_last=gl, x0=x0,
+                                                        gate=so.SIGMOID)
+        s, t = x0.clone(), gl.clone()
+        y, s2 = deeppcr.deeppcr_gated_scan_forward(a, u, x0=s, x_last=s, gate=so.SIGMOID)
+        deeppcr.deeppcr_gated_scan_backward(a, u, x, g, g_last=t, x0=x0, dx0=t, gate=so.SIGMOID)
+        assert s2 is s and torch.equal(s, last) and torch.equal(y, x) and torch.equal(t, dx0)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("shape", [(1, 1), (3, 5), (2, 64), (256, 130), (1, 4096), (9, 1001)], ids=str)
+def test_step(dev, kind, shape):
+    """Steps one after the other are the rows of the forward pass."""
+    B, w = shape
+    for gate in (so.DIRECT, so.SIGMOID):
+        a, u, _, x0, _ = inputs(B, 6, w, gate, TYPES[kind], dev)
+        rx, _ = so.scan_forward(cpu(a), cpu(u), cpu(x0), None, gate)
+        s, q = so.gates(cpu(a), gate)
+        before = np.concatenate([cpu(x0)[:, None], rx[:, :-1]], axis=1)
+        e = bound_of(s, np.abs(s * before) + np.abs(q * cpu(u)))
+        state = x0.clone()
+        for l in range(6):
+            if l == 3:      # the old state stays
+                old, state = state.clone(), torch.empty_like(state)
+                keep = old.clone()
+                x = deeppcr.deeppcr_gated_scan_step(a[:, l], u[:, l], old, gate=gate,
+                                                    state_out=state)
+                assert torch.equal(old, keep)
+            else:
+                x = deeppcr.deeppcr_gated_scan_step(a[:, l], u[:, l], state, gate=gate)
+            check(state, rx[:, l], e[:, l], torch.float32, "state")
+            check(x, rx[:, l], e[:, l], TYPES[kind], "x")
+
+
+def test_same_bits_every_time(dev):
+    for size in ((1, 9000, 70), (4, 1000, 256)):
+        a, u, g, x0, gl = inputs(*size, so.SIGMOID, torch.bfloat16, dev)
+        def run():
+            x, last = deeppcr.deeppcr_gated_scan_forward(a, u, x0=x0, gate=so.SIGMOID)
+            return [x, last, *deeppcr.deeppcr_gated_scan_backward(a, u, x, g, g_last=gl, x0=x0,
+                                                                  gate=so.SIGMOID)]
+        first = run()
+        for _ in range(5):
+            assert all(torch.equal(p, q) for p, q in zip(first, run()))
+
+
+def test_on_another_stream_and_captured(dev):
+    """A captured forward and backward, replayed between eager calls on other
+    data, two graphs on one pool, and calls on a stream of their own."""
+    a, u, g, x0, gl = inputs(2, 1500, 64, so.SIGMOID, torch.bfloat16, dev)
+    x = torch.empty_like(a)
+    last, dx0 = torch.empty_like(x0), torch.empty_like(x0)
+    da, du = torch.empty_like(a), torch.empty_like(a)
+    ws = torch.empty(deeppcr.gated_scan_workspace_bytes(2, 1500, 64), dtype=torch.uint8,
+                     device=dev)
+
+    def run():
+        deeppcr.deeppcr_gated_scan_forward(a, u, x0=x0, gate=so.SIGMOID, x=x, x_last=last,
+                                           workspace=ws)
+        deeppcr.deeppcr_gated_scan_backward(a, u, x, g, g_last=gl, x0=x0, gate=so.SIGMOID, da=da,
+                                            du=du, dx0=dx0, workspace=ws)
+
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    side = torch.cuda.Stream()
+    for k in range(4):
+        a.copy_(torch.randn_like(a)), u.copy_(torch.randn_like(a)), g.copy_(torch.randn_like(a))
+        want = [*deeppcr.deeppcr_gated_scan_forward(a, u, x0=x0, gate=so.SIGMOID)]
+        want += deeppcr.deeppcr_gated_scan_backward(a, u, want[0], g, g_last=gl, x0=x0,
+                                                    gate=so.SIGMOID)
+        for t in (x, last, da, du, dx0):
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(want, (x, last, da, du, dx0)))
+        side.wait_stream(torch.cuda.current_stream())
+        got = deeppcr.deeppcr_gated_scan_forward(a, u, x0=x0, gate=so.SIGMOID, stream=side)
+        side.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(want, got))

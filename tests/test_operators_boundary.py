@@ -1,0 +1,91 @@
+"""The operators of recurrent language models reject invalid arguments before
+any HIP call (so these run without a GPU)."""
+import ctypes
+
+import pytest
+
+from paper_2309_16318_amd import deeppcr
+
+E = deeppcr.EINVAL
+# Fake, non-overlapping "device" addresses: validation must reject before use.
+P = [ctypes.c_void_p(0x10000000 * (i + 1)) for i in range(16)]
+BIG = 1 << 40
+
+
+def off(p, n):
+    return ctypes.c_void_p(p.value + n)
+
+
+def _fwd(a=P[0], lda=40, u=P[1], ldu=40, x0=P[2], ln=P[3], x=P[4], last=P[5], B=2, L=8, w=40,
+         gate=1, dtype=1, ws=P[6], nws=BIG):
+    return deeppcr.lib().deeppcr_gated_scan_forward(a, lda, u, ldu, x0, ln, x, last, B, L, w, gate,
+                                                    dtype, ws, nws, None)
+
+
+def _bwd(a=P[0], lda=40, u=P[1], ldu=40, x=P[2], x0=P[3], ln=P[4], g=P[5], ldg=40, gl=P[6],
+         da=P[7], du=P[8], dx0=P[9], B=2, L=8, w=40, gate=1, dtype=1, ws=P[10], nws=BIG):
+    return deeppcr.lib().deeppcr_gated_scan_backward(a, lda, u, ldu, x, x0, ln, g, ldg, gl, da, du,
+                                                     dx0, B, L, w, gate, dtype, ws, nws, None)
+
+
+def _step(a=P[0], lda=40, u=P[1], ldu=40, s=P[2], so=P[3], x=P[4], B=2, w=40, gate=1, dtype=1):
+    return deeppcr.lib().deeppcr_gated_scan_step(a, lda, u, ldu, s, so, x, B, w, gate, dtype, None)
+
+
+def test_gated_scan_sizes():
+    f = deeppcr.gated_scan_workspace_bytes
+    assert f(1, 1, 1) > 0 and f(8, 65536, 1024) > 0
+    for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (-1, 4, 4), (1 << 20, 4, 1 << 11)):
+        assert f(*bad) == 0
+
+
+@pytest.mark.parametrize("call,required,arrays", [
+    (_fwd, "a u x ws", "a u x0 ln x last ws"),
+    (_bwd, "a u x g da du ws", "a u x x0 ln g gl da du dx0 ws"),
+    (_step, "a u s so", "a u s so x"),
+])
+def test_gated_scan_rejects_invalid_arguments(call, required, arrays):
+    import inspect
+    default = {k: v.default for k, v in inspect.signature(call).parameters.items()}
+    for k in required.split():
+        assert call(**{k: None}) == E, k
+    for k in arrays.split():
+        # sequences with a row stride start at any element, the rest at 16 bytes
+        for n in (1, 3) if "ld" + k in default else (4, 8):
+            assert call(**{k: off(default[k], n)}) == E, k
+    for bad in (dict(B=0), dict(B=-1), dict(w=0), dict(gate=2), dict(gate=-1), dict(dtype=3),
+                dict(dtype=-1), dict(lda=39), dict(ldu=39), dict(lda=-40),
+                dict(B=1 << 20, w=1 << 11, lda=1 << 11, ldu=1 << 11, ldg=1 << 11)):
+        if call is not _bwd:
+            bad.pop("ldg", None)
+        assert call(**bad) == E, bad
+    if call is not _step:
+        assert call(L=0) == E
+        assert call(nws=deeppcr.gated_scan_workspace_bytes(2, 8, 40) - 1) == deeppcr.EWORKSPACE
+
+
+def test_gated_scan_rejects_overlaps():
+    for out in ("x", "last", "ws"):
+        for other in (P[0], P[1], off(P[2], 16), P[3], off(P[0], 2 * 8 * 40 * 2 - 16)):
+            assert _fwd(**{out: other}) == E, (out, other)
+    assert _fwd(last=off(P[4], 16)) == E                # x_last over x
+    assert _fwd(ws=P[5]) == E                           # workspace over x_last
+    # a strided input reaches to its last row's end
+    assert _fwd(lda=400, x=off(P[0], (15 * 400 + 40) * 2 - 16)) == E
+    for out in ("da", "du", "dx0", "ws"):
+        for other in (P[0], P[1], P[2], P[3], P[4], P[5], off(P[6], 16)):
+            assert _bwd(**{out: other}) == E, (out, other)
+    assert _bwd(da=P[8]) == E and _bwd(dx0=P[8]) == E and _bwd(ldg=39) == E
+    assert _step(so=off(P[2], 16)) == E and _step(x=P[0]) == E and _step(x=P[3]) == E
+    assert _step(so=P[1]) == E
+
+
+def test_binding_rejects_what_is_not_a_gpu_sequence():
+    torch = pytest.importorskip("torch")
+    a = torch.zeros(2, 3, 4)
+    with pytest.raises(ValueError):
+        deeppcr.deeppcr_gated_scan_forward(a, a)                    # on the CPU
+    with pytest.raises(ValueError):
+        deeppcr.deeppcr_gated_scan_forward(a.double(), a.double())  # no such type
+    with pytest.raises(ValueError):
+        deeppcr.deeppcr_gated_scan_step(a[:, 0], a[:, 0], a[:, 0])
