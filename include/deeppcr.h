@@ -401,7 +401,10 @@ int deeppcr_seq_backward(const float* W, const float* bias, const float* z0, con
 enum { DEEPPCR_F32 = 0, DEEPPCR_BF16 = 1, DEEPPCR_F16 = 2 };
 enum {
     DEEPPCR_GATE_DIRECT = 0,   /* scan: a is the multiplier itself               */
-    DEEPPCR_GATE_SIGMOID = 1   /* sigmoid of the gate's argument                 */
+    DEEPPCR_GATE_NONE = 0,     /* residual norm: no gate                         */
+    DEEPPCR_GATE_SIGMOID = 1,  /* sigmoid of the gate's argument                 */
+    DEEPPCR_GATE_SILU = 2,     /* z sigmoid(z) (residual norm)                   */
+    DEEPPCR_GATE_LINEAR = 3    /* z itself (residual norm)                       */
 };
 
 /*
@@ -466,6 +469,57 @@ int deeppcr_gated_scan_step(const void* a, long long lda, const void* u, long lo
                             const float* state, float* state_out, void* x, int B, int w,
                             int gate, int dtype, void* stream);
 
+/* Largest width of the residual norm. */
+#define DEEPPCR_MAX_NORM_WIDTH 8192
+
+/*
+ * What stands between two blocks of a residual stack, in one pass over the
+ * rows: the norm behind the block, its gate and residual scale, the addition
+ * to the stream and the norm in front of the next block.  For every row
+ *   yn = w_post * y * rstd_post,          rstd_post = 1 / sqrt(mean(y^2) + eps)
+ *   x_out = x + scale * act(z) * yn
+ *   h = w_pre * x_out * rstd_pre,         rstd_pre = 1 / sqrt(mean(x_out^2) + eps)
+ * each over the w channels; h is formed from x_out before its rounding.
+ *   x [B, L, w] the stream;  y [B, L, w] the block's output, row stride ldy,
+ *         or NULL: there is none, and h is the norm of x (the front of a
+ *         stack; z, w_post, scale, x_out have to be NULL, gate NONE)
+ *   gate  a DEEPPCR_GATE_* value; z its argument: [B, L, w] with row stride
+ *         ldz, or with z_per_seq = 1 [B, w], one row for all of a sequence
+ *         (row stride ldz); NULL for DEEPPCR_GATE_NONE
+ *   w_post [w] or NULL: y is not normalised;  scale [w] or NULL: one
+ *   w_pre  [w] or NULL: there is no norm in front (h has to be NULL)
+ *   x_out [B, L, w], h [B, L, w] outputs; x_out may be x
+ *   rstd_post, rstd_pre [B, L] float32, outputs for the backward pass, or NULL
+ * eps >= 0 and finite; 1 <= w <= DEEPPCR_MAX_NORM_WIDTH; with z_per_seq at
+ * most 2^23 sequences.
+ */
+int deeppcr_residual_norm_forward(const void* x, const void* y, long long ldy, const void* z,
+                                  long long ldz, const float* w_post, const float* scale,
+                                  const float* w_pre, void* x_out, void* h, float* rstd_post,
+                                  float* rstd_pre, int B, int L, int w, int gate, int z_per_seq,
+                                  float eps, int dtype, void* stream);
+
+/*
+ * Its backward pass from the same inputs and rstd_post, rstd_pre of the
+ * forward pass, for dx_out = dLoss/dx_out (NULL: zero) and dh = dLoss/dh
+ * (NULL if and only if w_pre is NULL):
+ *   dx, dy [B, L, w], dz like z (contiguous; summed over a sequence's rows
+ *   where z_per_seq = 1) of type dtype; dw_post, dscale, dw_pre [w] float32,
+ *   summed over all rows, each NULL where it is not wanted or its weight is
+ *   NULL.  With y NULL: dx and dw_pre only, dy and dz NULL.
+ * workspace_bytes >= deeppcr_residual_norm_workspace_bytes(B, L, w, z_per_seq),
+ * 0 for invalid sizes.
+ */
+size_t deeppcr_residual_norm_workspace_bytes(int B, int L, int w, int z_per_seq);
+int deeppcr_residual_norm_backward(const void* x, const void* y, long long ldy, const void* z,
+                                   long long ldz, const float* w_post, const float* scale,
+                                   const float* w_pre, const float* rstd_post,
+                                   const float* rstd_pre, const void* dx_out, const void* dh,
+                                   void* dx, void* dy, void* dz, float* dw_post, float* dscale,
+                                   float* dw_pre, int B, int L, int w, int gate, int z_per_seq,
+                                   int dtype, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+
 /*
  * Instrumentation (not part of the numerical path).  While enabled, the
  * library brackets its kernel launches with HIP events on the launch's own
@@ -487,7 +541,8 @@ enum {
     DEEPPCR_KCLASS_SEQUENTIAL = 5, /* sequential baseline passes               */
     DEEPPCR_KCLASS_PCR_TAIL = 6,   /* substitution inside chunks, or row by row */
     DEEPPCR_KCLASS_SCAN = 7,       /* gated scan                               */
-    DEEPPCR_KCLASS_COUNT = 8
+    DEEPPCR_KCLASS_NORM = 8,       /* residual norm                            */
+    DEEPPCR_KCLASS_COUNT = 9
 };
 int deeppcr_profile_enable(int on);
 /* Times only the classes whose bit (1 << class) is set in `class_mask` (all

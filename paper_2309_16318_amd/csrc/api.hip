@@ -1530,6 +1530,20 @@ bool clash(std::initializer_list<Extent> ins, std::initializer_list<Extent> outs
     return false;
 }
 
+bool norm_ok(int B, int L, int w, int z_per_seq, int dtype) {
+    return seq_ok(B, L, w, dtype) && w <= DEEPPCR_MAX_NORM_WIDTH &&
+           (z_per_seq == 0 || (z_per_seq == 1 && B <= (1 << 23)));
+}
+
+// Without y there is nothing for the gate, the scale or the norm behind to act on.
+bool norm_pieces_ok(const void* x, const void* y, const void* z, const float* w_post,
+                    const float* scale, int gate, int z_per_seq) {
+    if (!x || gate < DEEPPCR_GATE_NONE || gate > DEEPPCR_GATE_LINEAR) return false;
+    if ((gate != DEEPPCR_GATE_NONE) != (z != nullptr)) return false;
+    if (!z && z_per_seq) return false;
+    return y || (!z && !w_post && !scale);
+}
+
 }  // namespace
 
 extern "C" {
@@ -1650,6 +1664,133 @@ int deeppcr_gated_scan_step(const void* a, long long lda, const void* u, long lo
         return launch_scan_step(a, lda, u, ldu, state, state_out, x, B, w, gate, dtype, st);
     });
     return err != hipSuccess ? hip_fail(err, "gated scan step") : DEEPPCR_OK;
+}
+
+size_t deeppcr_residual_norm_workspace_bytes(int B, int L, int w, int z_per_seq) {
+    return norm_ok(B, L, w, z_per_seq, DEEPPCR_F32) ? norm_workspace(B, w, z_per_seq) : 0;
+}
+
+int deeppcr_residual_norm_forward(const void* x, const void* y, long long ldy, const void* z,
+                                  long long ldz, const float* w_post, const float* scale,
+                                  const float* w_pre, void* x_out, void* h, float* rstd_post,
+                                  float* rstd_pre, int B, int L, int w, int gate, int z_per_seq,
+                                  float eps, int dtype, void* stream) {
+    const SpanGuard span_guard;
+    if (!norm_ok(B, L, w, z_per_seq, dtype) || !std::isfinite(eps) || eps < 0.f)
+        return DEEPPCR_EINVAL;
+    if (!norm_pieces_ok(x, y, z, w_post, scale, gate, z_per_seq)) return DEEPPCR_EINVAL;
+    // the outputs that the pieces have, and no others
+    if ((y != nullptr) != (x_out != nullptr) || (w_pre != nullptr) != (h != nullptr) ||
+        (!y && !h) || (rstd_post && !w_post) || (rstd_pre && !w_pre))
+        return DEEPPCR_EINVAL;
+    const int e = elem_size(dtype);
+    const double rows = (double)B * L, zrows = z_per_seq ? B : rows;
+    if (!on_element({y, z}, e) ||
+        !aligned({x, w_post, scale, w_pre, x_out, h, rstd_post, rstd_pre}))
+        return DEEPPCR_EINVAL;
+    if ((y && !stride_ok(rows, w, ldy, e)) || (z && !stride_ok(zrows, w, ldz, e)))
+        return DEEPPCR_EINVAL;
+    const size_t nw = (size_t)w * 4, nr = (size_t)rows * 4;
+    if (clash({extent(x, rows, w, w, e), extent(y, rows, w, ldy, e), extent(z, zrows, w, ldz, e),
+               {w_post, nw}, {scale, nw}, {w_pre, nw}},
+              {extent(x_out, rows, w, w, e), extent(h, rows, w, w, e), {rstd_post, nr},
+               {rstd_pre, nr}},
+              {x, nullptr, nullptr, nullptr}))
+        return DEEPPCR_EINVAL;
+    NormArgs k{};
+    k.x = x;
+    k.y = y;
+    k.ldy = ldy;
+    k.z = z;
+    k.ldz = ldz;
+    k.w_post = w_post;
+    k.scale = scale;
+    k.w_pre = w_pre;
+    k.x_out = x_out;
+    k.h = h;
+    k.rstd_post = rstd_post;
+    k.rstd_pre = rstd_pre;
+    k.B = B;
+    k.L = L;
+    k.w = w;
+    k.gate = gate;
+    k.z_per_seq = z_per_seq;
+    k.eps = eps;
+    hipStream_t st = (hipStream_t)stream;
+    const double n = rows * w;
+    const double bytes = n * e * (1 + (y ? 2 : 0) + (h ? 1 : 0)) + (z ? zrows * w * e : 0.0);
+    const hipError_t err = timed(DEEPPCR_KCLASS_NORM, bytes, 12.0 * n, st,
+                                 [&] { return launch_norm_fwd(k, dtype, st); });
+    return err != hipSuccess ? hip_fail(err, "residual norm") : DEEPPCR_OK;
+}
+
+int deeppcr_residual_norm_backward(const void* x, const void* y, long long ldy, const void* z,
+                                   long long ldz, const float* w_post, const float* scale,
+                                   const float* w_pre, const float* rstd_post,
+                                   const float* rstd_pre, const void* dx_out, const void* dh,
+                                   void* dx, void* dy, void* dz, float* dw_post, float* dscale,
+                                   float* dw_pre, int B, int L, int w, int gate, int z_per_seq,
+                                   int dtype, void* workspace, size_t workspace_bytes,
+                                   void* stream) {
+    const SpanGuard span_guard;
+    if (!workspace || !dx || !norm_ok(B, L, w, z_per_seq, dtype)) return DEEPPCR_EINVAL;
+    if (!norm_pieces_ok(x, y, z, w_post, scale, gate, z_per_seq)) return DEEPPCR_EINVAL;
+    if ((y != nullptr) != (dy != nullptr) || (z != nullptr) != (dz != nullptr) ||
+        (w_pre != nullptr) != (dh != nullptr) || (w_pre && !rstd_pre) ||
+        (w_post && !rstd_post) || (!dx_out && !dh))
+        return DEEPPCR_EINVAL;
+    if ((dw_post && !w_post) || (dscale && !scale) || (dw_pre && !w_pre)) return DEEPPCR_EINVAL;
+    const int e = elem_size(dtype);
+    const double rows = (double)B * L, zrows = z_per_seq ? B : rows;
+    if (!on_element({y, z}, e) ||
+        !aligned({x, w_post, scale, w_pre, rstd_post, rstd_pre, dx_out, dh, dx, dy, dz, dw_post,
+                  dscale, dw_pre, workspace}))
+        return DEEPPCR_EINVAL;
+    if ((y && !stride_ok(rows, w, ldy, e)) || (z && !stride_ok(zrows, w, ldz, e)))
+        return DEEPPCR_EINVAL;
+    const size_t need = norm_workspace(B, w, z_per_seq);
+    if (workspace_bytes < need) return DEEPPCR_EWORKSPACE;
+    const size_t nw = (size_t)w * 4, nr = (size_t)rows * 4;
+    if (clash({extent(x, rows, w, w, e), extent(y, rows, w, ldy, e), extent(z, zrows, w, ldz, e),
+               {w_post, nw}, {scale, nw}, {w_pre, nw}, {rstd_post, nr}, {rstd_pre, nr},
+               extent(dx_out, rows, w, w, e), extent(dh, rows, w, w, e)},
+              {extent(dx, rows, w, w, e), extent(dy, rows, w, w, e), extent(dz, zrows, w, w, e),
+               {dw_post, nw}, {dscale, nw}, {dw_pre, nw}, {workspace, need}},
+              {nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr}))
+        return DEEPPCR_EINVAL;
+    NormArgs k{};
+    k.x = x;
+    k.y = y;
+    k.ldy = ldy;
+    k.z = z;
+    k.ldz = ldz;
+    k.w_post = w_post;
+    k.scale = scale;
+    k.w_pre = w_pre;
+    // read only
+    k.rstd_post = const_cast<float*>(rstd_post);
+    k.rstd_pre = const_cast<float*>(rstd_pre);
+    k.dx_out = dx_out;
+    k.dh = dh;
+    k.dx = dx;
+    k.dy = dy;
+    k.dz = dz;
+    k.dw_post = dw_post;
+    k.dscale = dscale;
+    k.dw_pre = dw_pre;
+    k.ws = workspace;
+    k.B = B;
+    k.L = L;
+    k.w = w;
+    k.gate = gate;
+    k.z_per_seq = z_per_seq;
+    hipStream_t st = (hipStream_t)stream;
+    const double n = rows * w;
+    const double bytes = n * e * (2 + (y ? 2 : 0) + (dx_out ? 1 : 0) + (dh ? 1 : 0)) +
+                         (z ? 2.0 * zrows * w * e : 0.0);
+    const hipError_t err = timed(DEEPPCR_KCLASS_NORM, bytes, 30.0 * n, st,
+                                 [&] { return launch_norm_bwd(k, dtype, st); });
+    return err != hipSuccess ? hip_fail(err, "residual norm backward") : DEEPPCR_OK;
 }
 
 void deeppcr_release_thread_state(void) {

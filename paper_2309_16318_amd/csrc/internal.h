@@ -391,4 +391,23 @@ hipError_t launch_scan_step(const void* a, long long lda, const void* u, long lo
                             const float* state, float* state_out, void* x, int B, int w, int gate,
                             int dtype, hipStream_t st);
 
+// ---------------------------------------------------------- residual norm
+struct NormArgs {
+    const void *x, *y, *z;          // [B, L, w]; y, z with row strides, or null
+    long long ldy, ldz;
+    const float *w_post, *scale, *w_pre;  // [w] or null
+    void *x_out, *h;                // forward
+    float *rstd_post, *rstd_pre;    // [B, L]; written by the forward pass, if not null
+    const void *dx_out, *dh;        // backward
+    void *dx, *dy, *dz;
+    float *dw_post, *dscale, *dw_pre;
+    void* ws;                       // norm_workspace bytes
+    float *part1, *part2;           // in it: sums of each workgroup
+    int B, L, w, gate, z_per_seq;
+    float eps;
+};
+size_t norm_workspace(int B, int w, bool z_per_seq);
+hipError_t launch_norm_fwd(const NormArgs& k, int dtype, hipStream_t st);
+hipError_t launch_norm_bwd(const NormArgs& k, int dtype, hipStream_t st);
+
 }  // namespace deeppcr

@@ -16,13 +16,15 @@ TANH_MLP, TANH_RESIDUAL, SIGMOID_MLP, SIGMOID_RESIDUAL, RELU_MLP, RELU_RESIDUAL 
 OP_PCR, OP_FWD, OP_BWD = 0, 1, 2
 ACT_TANH, ACT_SIGMOID, ACT_RELU = 0, 1, 2
 F32, BF16, F16 = range(3)
-GATE_DIRECT, GATE_SIGMOID = 0, 1
+GATE_DIRECT = GATE_NONE = 0
+GATE_SIGMOID, GATE_SILU, GATE_LINEAR = 1, 2, 3
 (KCLASS_PCR_LEVEL, KCLASS_LAYER, KCLASS_UPDATE, KCLASS_WGRAD, KCLASS_OTHER, KCLASS_SEQUENTIAL,
- KCLASS_PCR_TAIL, KCLASS_SCAN) = range(8)
+ KCLASS_PCR_TAIL, KCLASS_SCAN, KCLASS_NORM) = range(9)
 KCLASS_NAMES = ("pcr_level", "layer", "update", "wgrad", "other", "sequential", "pcr_tail",
-                "scan")
+                "scan", "norm")
 MAX_WIDTH = 1024
 MAX_BLOCK_WIDTH = 128  # collapsed-skip ResNet and the chunked solve
+MAX_NORM_WIDTH = 8192
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdeeppcr.so")
 
@@ -82,6 +84,14 @@ SIGNATURES = {
                                     [_c.c_int] * 5 + [_c.c_void_p, _c.c_size_t, _c.c_void_p]),
     "deeppcr_gated_scan_step": (_c.c_int, [_c.c_void_p, _c.c_longlong] * 2 + [_c.c_void_p] * 3 +
                                 [_c.c_int] * 4 + [_c.c_void_p]),
+    "deeppcr_residual_norm_workspace_bytes": (_c.c_size_t, [_c.c_int] * 4),
+    "deeppcr_residual_norm_forward": (_c.c_int, [_c.c_void_p] +
+                                      [_c.c_void_p, _c.c_longlong] * 2 + [_c.c_void_p] * 7 +
+                                      [_c.c_int] * 5 + [_c.c_float, _c.c_int, _c.c_void_p]),
+    "deeppcr_residual_norm_backward": (_c.c_int, [_c.c_void_p] +
+                                       [_c.c_void_p, _c.c_longlong] * 2 + [_c.c_void_p] * 13 +
+                                       [_c.c_int] * 6 +
+                                       [_c.c_void_p, _c.c_size_t, _c.c_void_p]),
     "deeppcr_profile_enable": (_c.c_int, [_c.c_int]),
     "deeppcr_profile_select": (_c.c_int, [_c.c_uint]),
     "deeppcr_profile_reset": (None, []),
@@ -634,6 +644,108 @@ def deeppcr_gated_scan_step(a, u, state, gate: int = GATE_DIRECT, x=None, state_
             (_ptr(a), lda, _ptr(u), ldu, _ptr(state), _ptr(state_out), _ptr(x), B, w, int(gate),
              dt), made)
     return x
+
+
+@dataclass
+class NormResult:
+    x_out: object
+    h: object
+    rstd_post: object
+    rstd_pre: object
+
+
+@dataclass
+class NormGrads:
+    dx: object
+    dy: object
+    dz: object
+    dw_post: object
+    dscale: object
+    dw_pre: object
+
+
+def residual_norm_workspace_bytes(B: int, L: int, w: int, z_per_seq: bool = False) -> int:
+    return int(lib().deeppcr_residual_norm_workspace_bytes(B, L, w, int(bool(z_per_seq))))
+
+
+def _norm_inputs(x, y, z, w_post, scale, w_pre):
+    """Checks the pieces; returns (dtype code, B, L, w, ldy, ldz, z_per_seq)."""
+    torch = _torch()
+    dt = _dtype_code(x, "x")
+    B, L, w = x.shape
+    _typed(x, (B, L, w), "x", x.dtype, x.device)
+    if not x.is_cuda:
+        raise ValueError("x must be a GPU tensor")
+    ldy = 0 if y is None else _rows(y, (B, L, w), "y", x)
+    per_seq = z is not None and z.dim() == 2
+    ldz = 0 if z is None else _rows(z, (B, w) if per_seq else (B, L, w), "z", x)
+    for t, n in ((w_post, "w_post"), (scale, "scale"), (w_pre, "w_pre")):
+        _typed(t, (w,), n, torch.float32, x.device)
+    return dt, B, L, w, ldy, ldz, int(per_seq)
+
+
+def deeppcr_residual_norm_forward(x, y=None, z=None, w_post=None, scale=None, w_pre=None,
+                                  gate: int = GATE_NONE, eps: float = 1e-6, x_out=None, h=None,
+                                  stream=None) -> NormResult:
+    """x_out = x + scale act(z) norm(y; w_post), h = norm(x_out; w_pre) over
+    [B, L, w]; each piece that is None is left out (without y: h = norm(x)).
+    z [B, L, w], or [B, w] for one gate per sequence."""
+    torch = _torch()
+    dt, B, L, w, ldy, ldz, per_seq = _norm_inputs(x, y, z, w_post, scale, w_pre)
+    made = []
+
+    def new(shape, dtype):
+        made.append(torch.empty(shape, dtype=dtype, device=x.device))
+        return made[-1]
+
+    if x_out is None and y is not None:
+        x_out = new((B, L, w), x.dtype)
+    if h is None and w_pre is not None:
+        h = new((B, L, w), x.dtype)
+    _typed(x_out, (B, L, w), "x_out", x.dtype, x.device)
+    _typed(h, (B, L, w), "h", x.dtype, x.device)
+    rpost = new((B, L), torch.float32) if w_post is not None else None
+    rpre = new((B, L), torch.float32) if w_pre is not None else None
+    _launch("deeppcr_residual_norm_forward", stream, x.device,
+            (_ptr(x), _ptr(y), ldy, _ptr(z), ldz, _ptr(w_post), _ptr(scale), _ptr(w_pre),
+             _ptr(x_out), _ptr(h), _ptr(rpost), _ptr(rpre), B, L, w, int(gate), per_seq,
+             float(eps), dt), made)
+    return NormResult(x_out if y is not None else x, h, rpost, rpre)
+
+
+def deeppcr_residual_norm_backward(x, y=None, rstd_post=None, rstd_pre=None, dx_out=None, dh=None,
+                                   z=None, w_post=None, scale=None, w_pre=None,
+                                   gate: int = GATE_NONE, dx=None, dy=None, dz=None,
+                                   workspace=None, stream=None) -> NormGrads:
+    """Gradients of the residual norm from its inputs, its statistics and
+    dx_out, dh; those of pieces that are None are None."""
+    torch = _torch()
+    dt, B, L, w, ldy, ldz, per_seq = _norm_inputs(x, y, z, w_post, scale, w_pre)
+    dev = x.device
+    for t, n in ((rstd_post, "rstd_post"), (rstd_pre, "rstd_pre")):
+        _typed(t, (B, L), n, torch.float32, dev)
+    made = []
+
+    def out(given, like, name, dtype=x.dtype):
+        if like is None:
+            return None
+        if given is None:
+            given = torch.empty(like.shape, dtype=dtype, device=dev)
+            made.append(given)
+        _typed(given, like.shape, name, dtype, dev)
+        return given
+
+    for t, n in ((dx_out, "dx_out"), (dh, "dh")):
+        _typed(t, (B, L, w), n, x.dtype, dev)
+    dx, dy, dz = out(dx, x, "dx"), out(dy, y, "dy"), out(dz, z, "dz")
+    dpost, dscale, dpre = (out(None, p, "", torch.float32) for p in (w_post, scale, w_pre))
+    ws, nbytes = _space(workspace, residual_norm_workspace_bytes(B, L, w, per_seq), dev, made)
+    _launch("deeppcr_residual_norm_backward", stream, dev,
+            (_ptr(x), _ptr(y), ldy, _ptr(z), ldz, _ptr(w_post), _ptr(scale), _ptr(w_pre),
+             _ptr(rstd_post), _ptr(rstd_pre), _ptr(dx_out), _ptr(dh), _ptr(dx), _ptr(dy),
+             _ptr(dz), _ptr(dpost), _ptr(dscale), _ptr(dpre), B, L, w, int(gate), per_seq, dt,
+             _ptr(ws), nbytes), made)
+    return NormGrads(dx, dy, dz, dpost, dscale, dpre)
 
 
 def release_thread_state() -> None:

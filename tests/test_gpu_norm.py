@@ -1,0 +1,225 @@
+"""Residual norm on the GPU against its float64 definition: types, gates, odd
+widths, pieces left out, strides, streams and captured graphs.
+
+Bounds, in float32 roundings (2^-24 relative each).  A row's sum of squares is
+added by 8 terms per thread and then over at most 20 levels or workgroup waves:
+28 roundings, half of that in its root; with the gate (at most 8) and the
+products 26 for the added term, so x_out errs by 26 roundings of |x| + |term|.
+The norm in front sees that error against the size of x_out: cond = | |x| +
+|term| | / |x_out| per row.  What follows is a short chain of such values: 64
+cond roundings of the terms' sizes; sums over rows add one rounding per row of
+a workgroup and per sixteenth of the workgroups, at most 128 here.  An output's
+rounding adds half a step of its type.
+"""
+import numpy as np
+import pytest
+
+from oracle import norm_oracle as no
+from paper_2309_16318_amd import deeppcr
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+E32 = 2.0 ** -24
+EPS = 1e-6
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+SIZES = [(1, 1, 1), (1, 2, 8), (2, 3, 5), (3, 70, 16), (1, 5, 100), (2, 7, 128), (1, 3, 511),
+         (2, 9, 512), (1, 5, 513), (2, 2, 520), (1, 3, 1000), (2, 33, 2048), (1, 3, 4100),
+         (1, 3, 8191), (1, 2, 8192), (3, 700, 24), (2, 1500, 64), (70, 3, 12)]
+
+
+@pytest.fixture(scope="module")
+def dev():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return torch.device("cuda:0")
+
+
+def cpu(t):
+    return None if t is None else t.detach().double().cpu().numpy()
+
+
+def check(got, ref, bound, dtype, what):
+    got, half = cpu(got), torch.finfo(dtype).eps / 2
+    tiny = torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+    assert got.shape == ref.shape, what
+    lim = bound * (1 + half) + half * np.abs(ref) + tiny
+    assert np.all(np.isfinite(got)), what
+    bad = np.abs(got - ref) - lim
+    assert np.max(bad) <= 0, (what, np.max(bad), np.unravel_index(np.argmax(bad), ref.shape))
+
+
+def inputs(B, L, w, gate, per_seq, dtype, dev, strided=False):
+    gen = torch.Generator().manual_seed(1000 * gate + 31 * B + 7 * L + w)
+    r = lambda *s: torch.randn(*s, generator=gen)
+    v = {k: r(B, L, w).to(dtype).to(dev) for k in ("x", "dx_out", "dh")}
+    if strided:
+        wide = torch.cat([3 * r(B, L, w), r(B, L, w), r(B, L, 8)], dim=2).to(dtype).to(dev)
+        v["y"], v["z"] = wide[..., :w], wide[..., w:2 * w]
+        if per_seq:
+            v["z"] = wide[:, 0, w:2 * w]
+    else:
+        v["y"] = (3 * r(B, L, w)).to(dtype).to(dev)
+        v["z"] = r(*((B, w) if per_seq else (B, L, w))).to(dtype).to(dev)
+    if gate == no.NONE:
+        v["z"] = None
+    for k in ("w_post", "scale", "w_pre"):
+        v[k] = (1 + 0.3 * r(w)).to(dev)
+    return v
+
+
+def both(v, gate, dtype, eps=EPS):
+    pieces = {k: v[k] for k in ("z", "w_post", "scale", "w_pre")}
+    f = deeppcr.deeppcr_residual_norm_forward(v["x"], v["y"], gate=gate, eps=eps, **pieces)
+    b = deeppcr.deeppcr_residual_norm_backward(v["x"], v["y"], f.rstd_post, f.rstd_pre,
+                                               dx_out=v["dx_out"], dh=v["dh"], gate=gate, **pieces)
+    torch.cuda.synchronize()
+    c = {k: cpu(t) for k, t in v.items()}
+    args = [c[k] for k in ("x", "y", "z", "w_post", "scale", "w_pre")]
+    out, h, rp, rq = no.norm_forward(*args, gate, eps)
+    x = c["x"]
+    row = lambda t: np.sqrt(np.sum(t * t, axis=-1, keepdims=True))
+    term = np.zeros_like(x)
+    if c["y"] is not None:
+        term = np.abs(out - x)
+        check(f.x_out, out, 26 * E32 * (np.abs(x) + term), dtype, "x_out")
+    size = np.abs(x) + term
+    cond = np.maximum(1, row(size) / np.maximum(row(out), 1e-300)) if rq is not None else 1.0
+    if rp is not None:
+        check(f.rstd_post, rp, 26 * E32 * rp, torch.float32, "rstd_post")
+    if rq is not None:
+        check(f.rstd_pre, rq, 64 * E32 * (cond * rq[..., None])[..., 0], torch.float32, "rstd_pre")
+        check(f.h, h, 64 * E32 * np.abs(c["w_pre"]) * rq[..., None] *
+              (size + cond * np.abs(out)), dtype, "h")
+    ref = no.norm_backward(*args, gate, eps, c["dx_out"], c["dh"])
+    mean = lambda t: np.mean(t, axis=-1, keepdims=True)
+    D = np.zeros_like(x) if c["dx_out"] is None else np.abs(c["dx_out"])
+    if rq is not None:
+        m, e = size * rq[..., None], np.abs(c["dh"] * c["w_pre"])
+        D = D + rq[..., None] * (e + m * mean(e * m))
+    u = 64 * E32 * cond
+    check(b.dx, ref[0], u * D, dtype, "dx")
+    sums = lambda t: np.sum((u + 128 * E32) * t, axis=(0, 1))
+    if rq is not None:
+        check(b.dw_pre, ref[5], sums(np.abs(c["dh"]) * size * rq[..., None]), torch.float32,
+              "dw_pre")
+    if c["y"] is None:
+        return f, b
+    wide = None if c["z"] is None else c["z"][:, None] if c["z"].ndim == 2 else c["z"]
+    val, slope = no.gate_values(gate, wide)
+    val = np.abs(val)
+    sc = 1.0 if c["scale"] is None else np.abs(c["scale"])
+    wp = 1.0 if c["w_post"] is None else np.abs(c["w_post"])
+    r = 1.0 if rp is None else rp[..., None]
+    n = np.abs(c["y"]) * r
+    dy = D * sc * wp * val
+    if rp is not None:
+        dy = r * (dy + n * mean(dy * n))
+    check(b.dy, ref[1], u * dy, dtype, "dy")
+    if wide is not None:
+        # the slope of z sigmoid(z) crosses zero: its terms' sizes
+        flat = np.abs(slope) if gate != no.SILU else no.sigmoid(wide) * (1 + np.abs(wide))
+        dz = D * sc * wp * n * flat
+        if c["z"].ndim == 2:
+            check(b.dz, ref[2], np.sum((u + 128 * E32) * dz, axis=1), dtype, "dz")
+        else:
+            check(b.dz, ref[2], u * dz, dtype, "dz")
+    if c["w_post"] is not None:
+        check(b.dw_post, ref[3], sums(D * val * n * sc), torch.float32, "dw_post")
+    if c["scale"] is not None:
+        check(b.dscale, ref[4], sums(D * val * n * wp), torch.float32, "dscale")
+    return f, b
+
+
+@pytest.mark.parametrize("size", SIZES, ids=str)
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_sizes(dev, size, kind):
+    for gate, per_seq in ((no.SILU, False), (no.SIGMOID, True)):
+        both(inputs(*size, gate, per_seq, TYPES[kind], dev), gate, TYPES[kind])
+
+
+@pytest.mark.parametrize("gate", [no.NONE, no.SIGMOID, no.SILU, no.LINEAR])
+@pytest.mark.parametrize("per_seq", [False, True])
+@pytest.mark.parametrize("without", ["", "w_post", "scale", "w_pre dh", "dx_out",
+                                     "y z w_post scale", "w_post scale w_pre dh"])
+def test_pieces_left_out(dev, gate, per_seq, without):
+    if gate == no.NONE and per_seq or gate != no.NONE and "y" in without.split():
+        pytest.skip("no gate to vary")
+    for size in ((2, 5, 40), (2, 3, 1030)):
+        v = inputs(*size, gate, per_seq, torch.float32, dev)
+        for k in without.split():
+            v[k] = None
+        f, b = both(v, gate, torch.float32)
+        if v["y"] is None:
+            assert f.x_out is v["x"] and b.dy is None and b.dz is None
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("size", [(2, 30, 48), (3, 7, 8), (1, 9, 41), (2, 3, 1024)], ids=str)
+def test_slices_of_a_projection(dev, kind, size):
+    for gate, per_seq in ((no.SILU, False), (no.LINEAR, True)):
+        v = inputs(*size, gate, per_seq, TYPES[kind], dev, strided=True)
+        assert v["y"].stride(1) == 2 * size[2] + 8
+        both(v, gate, TYPES[kind])
+
+
+def test_zero_rows_and_eps(dev):
+    """A row of zeros stays finite, with its gradient; eps counts."""
+    v = inputs(2, 6, 64, no.SILU, False, torch.float32, dev)
+    v["y"][0, 2] = 0
+    v["x"][1, 3] = 0
+    v["y"][1, 3] = 0
+    both(v, no.SILU, torch.float32)
+    both(v, no.SILU, torch.float32, eps=0.5)
+
+
+def test_stream_in_place(dev):
+    v = inputs(2, 9, 1000, no.SILU, False, torch.bfloat16, dev)
+    p = {k: v[k] for k in ("z", "w_post", "scale", "w_pre")}
+    f = deeppcr.deeppcr_residual_norm_forward(v["x"], v["y"], gate=no.SILU, **p)
+    x = v["x"].clone()
+    g = deeppcr.deeppcr_residual_norm_forward(x, v["y"], gate=no.SILU, x_out=x, **p)
+    assert g.x_out is x and torch.equal(x, f.x_out) and torch.equal(g.h, f.h)
+
+
+def test_a_nan_stays_in_its_row(dev):
+    for w in (48, 1100):
+        v = inputs(2, 40, w, no.SILU, False, torch.bfloat16, dev)
+        p = {k: v[k] for k in ("z", "w_post", "scale", "w_pre")}
+        f = deeppcr.deeppcr_residual_norm_forward(v["x"], v["y"], gate=no.SILU, **p)
+        v["y"][1, 7, 5] = float("nan")
+        g = deeppcr.deeppcr_residual_norm_forward(v["x"], v["y"], gate=no.SILU, **p)
+        keep = torch.ones(2, 40, dtype=torch.bool, device=dev)
+        keep[1, 7] = False
+        assert torch.equal(f.h[keep], g.h[keep]) and torch.equal(f.x_out[keep], g.x_out[keep])
+        assert torch.isnan(g.h[1, 7]).all()
+
+
+@pytest.mark.parametrize("per_seq", [False, True])
+def test_same_bits_every_time_and_captured(dev, per_seq):
+    v = inputs(3, 400, 96, no.SILU, per_seq, torch.bfloat16, dev)
+    p = {k: v[k] for k in ("z", "w_post", "scale", "w_pre")}
+
+    def run():
+        f = deeppcr.deeppcr_residual_norm_forward(v["x"], v["y"], gate=no.SILU, **p)
+        b = deeppcr.deeppcr_residual_norm_backward(v["x"], v["y"], f.rstd_post, f.rstd_pre,
+                                                   dx_out=v["dx_out"], dh=v["dh"], gate=no.SILU,
+                                                   **p)
+        return [f.x_out, f.h, b.dx, b.dy, b.dz, b.dw_post, b.dscale, b.dw_pre]
+
+    first = run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept = run()
+    for k in range(4):
+        if k:
+            v["x"].copy_(torch.randn_like(v["x"]))
+            v["dh"].copy_(torch.randn_like(v["x"]))
+        want = run()
+        for t in kept:
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(s, t) for s, t in zip(want, kept))
+        if k == 0:
+            assert all(torch.equal(s, t) for s, t in zip(want, first))

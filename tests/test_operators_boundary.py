@@ -89,3 +89,65 @@ def test_binding_rejects_what_is_not_a_gpu_sequence():
         deeppcr.deeppcr_gated_scan_forward(a.double(), a.double())  # no such type
     with pytest.raises(ValueError):
         deeppcr.deeppcr_gated_scan_step(a[:, 0], a[:, 0], a[:, 0])
+
+
+def _nfwd(x=P[0], y=P[1], ldy=40, z=P[2], ldz=40, post=P[3], sc=P[4], pre=P[5], xo=P[6], h=P[7],
+          rp=P[8], rq=P[9], B=2, L=8, w=40, gate=2, per=0, eps=1e-6, dtype=1):
+    return deeppcr.lib().deeppcr_residual_norm_forward(x, y, ldy, z, ldz, post, sc, pre, xo, h, rp,
+                                                       rq, B, L, w, gate, per, eps, dtype, None)
+
+
+def _nbwd(x=P[0], y=P[1], ldy=40, z=P[2], ldz=40, post=P[3], sc=P[4], pre=P[5], rp=P[6], rq=P[7],
+          dxo=P[8], dh=P[9], dx=P[10], dy=P[11], dz=P[12], dpost=P[13], dsc=P[14], dpre=P[15],
+          B=2, L=8, w=40, gate=2, per=0, dtype=1, ws=off(P[15], 1 << 27), nws=BIG):
+    return deeppcr.lib().deeppcr_residual_norm_backward(
+        x, y, ldy, z, ldz, post, sc, pre, rp, rq, dxo, dh, dx, dy, dz, dpost, dsc, dpre, B, L, w,
+        gate, per, dtype, ws, nws, None)
+
+
+def test_residual_norm_sizes():
+    f = deeppcr.residual_norm_workspace_bytes
+    assert f(2, 8, 40) > 0 and f(2, 8, 40, True) > 0 and f(1, 1, deeppcr.MAX_NORM_WIDTH) > 0
+    for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1, 1, 8193), ((1 << 23) + 1, 1, 8, True)):
+        assert f(*bad) == 0
+    assert deeppcr.lib().deeppcr_residual_norm_workspace_bytes(1, 1, 8, 2) == 0
+
+
+def test_residual_norm_rejects_invalid_arguments():
+    for call, arrays, strided in (
+            (_nfwd, "x post sc pre xo h rp rq", "y z"),
+            (_nbwd, "x post sc pre rp rq dxo dh dx dy dz dpost dsc dpre ws", "y z")):
+        import inspect
+        default = {k: v.default for k, v in inspect.signature(call).parameters.items()}
+        for k in arrays.split():
+            assert call(**{k: off(default[k], 8)}) == E, k
+        for k in strided.split():
+            assert call(**{k: off(default[k], 1)}) == E, k
+        for bad in (dict(x=None), dict(B=0), dict(L=0), dict(w=0), dict(w=8193), dict(gate=4),
+                    dict(gate=-1), dict(gate=0), dict(z=None), dict(z=None, gate=0, per=1),
+                    dict(per=2), dict(dtype=3), dict(ldy=39), dict(ldz=39), dict(y=None),
+                    dict(pre=None), dict(per=1, B=(1 << 23) + 1)):
+            assert call(**bad) == E, bad
+    assert _nfwd(xo=None) == E and _nfwd(h=None) == E
+    assert _nfwd(post=None) == E                # its statistics are asked for
+    for eps in (-1.0, float("nan"), float("inf")):
+        assert _nfwd(eps=eps) == E
+    assert _nfwd(y=None, z=None, gate=0, post=None, sc=None, xo=None, rp=None, pre=None, h=None,
+                 rq=None) == E                  # nothing to do
+    for k in ("rp", "rq", "dx", "dy", "dz", "ws", "dh"):
+        assert _nbwd(**{k: None}) == E, k
+    assert _nbwd(dxo=None, dh=None, pre=None, dpre=None) == E     # no gradient comes in
+    assert _nbwd(sc=None) == E and _nbwd(post=None) == E          # gradient of a missing weight
+    need = deeppcr.residual_norm_workspace_bytes(2, 8, 40)
+    assert _nbwd(nws=need - 1) == deeppcr.EWORKSPACE
+
+
+def test_residual_norm_rejects_overlaps():
+    for out in ("h", "rp", "rq"):
+        for other in (P[0], P[1], P[2], P[3], P[4], P[5], P[6]):
+            assert _nfwd(**{out: other}) == E, out
+    assert _nfwd(xo=off(P[0], 16)) == E and _nfwd(xo=P[1]) == E
+    for out in ("dx", "dy", "dz", "dpost", "dsc", "dpre", "ws"):
+        for i in range(10):
+            assert _nbwd(**{out: P[i]}) == E, (out, i)
+    assert _nbwd(dx=P[11]) == E and _nbwd(ws=P[13]) == E
