@@ -520,6 +520,32 @@ int deeppcr_residual_norm_backward(const void* x, const void* y, long long ldy, 
                                    int dtype, void* workspace, size_t workspace_bytes,
                                    void* stream);
 
+/* Largest side of an orthogonalised matrix. */
+#define DEEPPCR_MAX_ORTHO_SIDE 8192
+
+/*
+ * Orthogonalised update of a stack of weight matrices from their gradients
+ * (dW of deeppcr_mlp_backward and deeppcr_resnet_backward is such a stack):
+ * for every matrix, X = G / (|G|_F + eps), then `steps` times
+ *   A = X X^T (X^T X where m > n),   X = ca X + (cb A + cc A A) X
+ * (X ca + X (cb A + cc A A)), a polynomial in the singular values that moves
+ * them towards one and leaves the singular vectors.  A zero matrix stays
+ * zero; a NaN or infinity stays in its matrix.
+ *   G [N, m, n], X [N, m, n] of type dtype, contiguous; X may be G
+ *   steps >= 0; ca, cb, cc finite, and such that the iterates stay moderate:
+ *         with s <= 1 the largest singular value, s and cb s^2 + cc s^4 have
+ *         to stay below 15 in every step for every s that can occur, else
+ *         DEEPPCR_EINVAL
+ *   eps   >= 0 and finite
+ * 1 <= m, n <= DEEPPCR_MAX_ORTHO_SIDE.
+ * workspace_bytes >= deeppcr_orthogonalize_workspace_bytes(N, m, n), 0 for
+ * invalid sizes.
+ */
+size_t deeppcr_orthogonalize_workspace_bytes(int N, int m, int n);
+int deeppcr_orthogonalize(const void* G, void* X, int N, int m, int n, int steps, float ca,
+                          float cb, float cc, float eps, int dtype, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
 /*
  * Instrumentation (not part of the numerical path).  While enabled, the
  * library brackets its kernel launches with HIP events on the launch's own
@@ -542,7 +568,8 @@ enum {
     DEEPPCR_KCLASS_PCR_TAIL = 6,   /* substitution inside chunks, or row by row */
     DEEPPCR_KCLASS_SCAN = 7,       /* gated scan                               */
     DEEPPCR_KCLASS_NORM = 8,       /* residual norm                            */
-    DEEPPCR_KCLASS_COUNT = 9
+    DEEPPCR_KCLASS_ORTHO = 9,      /* orthogonalised update                    */
+    DEEPPCR_KCLASS_COUNT = 10
 };
 int deeppcr_profile_enable(int on);
 /* Times only the classes whose bit (1 << class) is set in `class_mask` (all

@@ -17,7 +17,7 @@ LIB = os.path.join(PKG, "libdeeppcr.so")
 
 SOURCES = ["api.hip", "layers.hip", "tiny.hip", "sequential.hip", "small.hip",
            "resnet.hip", "chunked.hip", "wide.hip", "panels.hip", "blocks.hip",
-           "scan.hip", "norm.hip"]
+           "scan.hip", "norm.hip", "ortho.hip"]
 ARCH = "gfx950"
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",

@@ -2,6 +2,7 @@
 // workspace carving, the PCR level loop and the Newton driver.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <cstdio>
@@ -1544,6 +1545,50 @@ bool norm_pieces_ok(const void* x, const void* y, const void* z, const float* w_
     return y || (!z && !w_post && !scale);
 }
 
+bool ortho_ok(int N, int m, int n, int dtype) {
+    return N >= 1 && m >= 1 && n >= 1 && m <= DEEPPCR_MAX_ORTHO_SIDE &&
+           n <= DEEPPCR_MAX_ORTHO_SIDE && dtype >= DEEPPCR_F32 && dtype <= DEEPPCR_F16 &&
+           (double)N * m * n < 2.0e17;
+}
+
+// Follows the largest singular value that an iterate can have: with s in
+// [0, top], |s (ca + q(s))| and q(s) = cb s^2 + cc s^4 take their largest
+// sizes at the ends or where a derivative vanishes (quadratics in s^2).  A
+// slack of 1/1000 stands for the rounding of the products.
+constexpr double kIterateLimit = 15.0;
+bool iterates_stay(int steps, double ca, double cb, double cc) {
+    if (!std::isfinite(ca) || !std::isfinite(cb) || !std::isfinite(cc)) return false;
+    double top = 1.0;
+    for (int i = 0; i < steps; ++i) {
+        top *= 1.001;
+        double s2[4] = {top * top, 0.0, 0.0, 0.0};
+        int n = 1;
+        // (ca s + cb s^3 + cc s^5)' = ca + 3 cb s^2 + 5 cc s^4,  q' ~ cb + 2 cc s^2
+        if (cc != 0.0) {
+            s2[n++] = -cb / (2.0 * cc);
+            const double disc = 9.0 * cb * cb - 20.0 * cc * ca;
+            if (disc >= 0.0) {
+                s2[n++] = (-3.0 * cb + std::sqrt(disc)) / (10.0 * cc);
+                s2[n++] = (-3.0 * cb - std::sqrt(disc)) / (10.0 * cc);
+            }
+        } else if (cb != 0.0) {
+            s2[n++] = -ca / (3.0 * cb);
+        }
+        double next = 0.0;
+        for (int j = 0; j < n; ++j) {
+            if (!(s2[j] >= 0.0) || s2[j] > top * top) continue;
+            const double q = (cb + cc * s2[j]) * s2[j], p = std::sqrt(s2[j]) * (ca + q);
+            if (!(std::fabs(q) < kIterateLimit) || !(std::fabs(p) < kIterateLimit) ||
+                !(top * top < kIterateLimit))
+                return false;
+            next = std::max(next, std::fabs(p));
+        }
+        // an iterate that shrank is still off by what rounding leaves
+        top = std::max(next, 1e-3);
+    }
+    return true;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1791,6 +1836,32 @@ int deeppcr_residual_norm_backward(const void* x, const void* y, long long ldy, 
     const hipError_t err = timed(DEEPPCR_KCLASS_NORM, bytes, 30.0 * n, st,
                                  [&] { return launch_norm_bwd(k, dtype, st); });
     return err != hipSuccess ? hip_fail(err, "residual norm backward") : DEEPPCR_OK;
+}
+
+size_t deeppcr_orthogonalize_workspace_bytes(int N, int m, int n) {
+    return ortho_ok(N, m, n, DEEPPCR_F32) ? ortho_workspace(N, m, n) : 0;
+}
+
+int deeppcr_orthogonalize(const void* G, void* X, int N, int m, int n, int steps, float ca,
+                          float cb, float cc, float eps, int dtype, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+    const SpanGuard span_guard;
+    if (!G || !X || !workspace || !ortho_ok(N, m, n, dtype) || steps < 0) return DEEPPCR_EINVAL;
+    if (!std::isfinite(eps) || eps < 0.f || !iterates_stay(steps, ca, cb, cc))
+        return DEEPPCR_EINVAL;
+    if (!aligned({G, X, workspace})) return DEEPPCR_EINVAL;
+    const size_t need = ortho_workspace(N, m, n);
+    if (workspace_bytes < need) return DEEPPCR_EWORKSPACE;
+    const size_t nx = (size_t)N * m * n * elem_size(dtype);
+    if (clash({{G, nx}}, {{X, nx}, {workspace, need}}, {G, nullptr})) return DEEPPCR_EINVAL;
+    hipStream_t st = (hipStream_t)stream;
+    const double k = m < n ? m : n, r = m < n ? n : m;
+    const hipError_t err =
+        timed(DEEPPCR_KCLASS_ORTHO, 2.0 * nx,
+              (double)N * steps * (k * (k + 1) * r + k * k * (k + 1) + 2 * k * k * r), st, [&] {
+            return launch_ortho(G, X, N, m, n, steps, ca, cb, cc, eps, dtype, workspace, st);
+        });
+    return err != hipSuccess ? hip_fail(err, "orthogonalize") : DEEPPCR_OK;
 }
 
 void deeppcr_release_thread_state(void) {

@@ -410,4 +410,9 @@ size_t norm_workspace(int B, int w, bool z_per_seq);
 hipError_t launch_norm_fwd(const NormArgs& k, int dtype, hipStream_t st);
 hipError_t launch_norm_bwd(const NormArgs& k, int dtype, hipStream_t st);
 
+// -------------------------------------------------- orthogonalised update
+size_t ortho_workspace(int N, int m, int n);
+hipError_t launch_ortho(const void* G, void* X, int N, int m, int n, int steps, float ca, float cb,
+                        float cc, float eps, int dtype, void* ws, hipStream_t st);
+
 }  // namespace deeppcr

@@ -19,12 +19,13 @@ F32, BF16, F16 = range(3)
 GATE_DIRECT = GATE_NONE = 0
 GATE_SIGMOID, GATE_SILU, GATE_LINEAR = 1, 2, 3
 (KCLASS_PCR_LEVEL, KCLASS_LAYER, KCLASS_UPDATE, KCLASS_WGRAD, KCLASS_OTHER, KCLASS_SEQUENTIAL,
- KCLASS_PCR_TAIL, KCLASS_SCAN, KCLASS_NORM) = range(9)
+ KCLASS_PCR_TAIL, KCLASS_SCAN, KCLASS_NORM, KCLASS_ORTHO) = range(10)
 KCLASS_NAMES = ("pcr_level", "layer", "update", "wgrad", "other", "sequential", "pcr_tail",
-                "scan", "norm")
+                "scan", "norm", "ortho")
 MAX_WIDTH = 1024
 MAX_BLOCK_WIDTH = 128  # collapsed-skip ResNet and the chunked solve
 MAX_NORM_WIDTH = 8192
+MAX_ORTHO_SIDE = 8192
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdeeppcr.so")
 
@@ -92,6 +93,9 @@ SIGNATURES = {
                                        [_c.c_void_p, _c.c_longlong] * 2 + [_c.c_void_p] * 13 +
                                        [_c.c_int] * 6 +
                                        [_c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "deeppcr_orthogonalize_workspace_bytes": (_c.c_size_t, [_c.c_int] * 3),
+    "deeppcr_orthogonalize": (_c.c_int, [_c.c_void_p] * 2 + [_c.c_int] * 4 + [_c.c_float] * 4 +
+                              [_c.c_int, _c.c_void_p, _c.c_size_t, _c.c_void_p]),
     "deeppcr_profile_enable": (_c.c_int, [_c.c_int]),
     "deeppcr_profile_select": (_c.c_int, [_c.c_uint]),
     "deeppcr_profile_reset": (None, []),
@@ -746,6 +750,34 @@ def deeppcr_residual_norm_backward(x, y=None, rstd_post=None, rstd_pre=None, dx_
              _ptr(dz), _ptr(dpost), _ptr(dscale), _ptr(dpre), B, L, w, int(gate), per_seq, dt,
              _ptr(ws), nbytes), made)
     return NormGrads(dx, dy, dz, dpost, dscale, dpre)
+
+
+def orthogonalize_workspace_bytes(N: int, m: int, n: int) -> int:
+    return int(lib().deeppcr_orthogonalize_workspace_bytes(N, m, n))
+
+
+def deeppcr_orthogonalize(G, X=None, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315),
+                          eps: float = 1e-7, workspace=None, stream=None):
+    """The orthogonalised update of a stack of gradients G [N, m, n] (or one,
+    [m, n]): Newton-Schulz steps of the polynomial `coeffs` on G / (|G| + eps);
+    X may be G."""
+    torch = _torch()
+    dt = _dtype_code(G, "G")
+    if not G.is_cuda or G.dim() not in (2, 3):
+        raise ValueError("G must be a GPU tensor [N, m, n] or [m, n]")
+    N, (m, n) = (1 if G.dim() == 2 else G.shape[0]), G.shape[-2:]
+    _typed(G, G.shape, "G", G.dtype, G.device)
+    made = []
+    if X is None:
+        X = torch.empty_like(G)
+        made.append(X)
+    _typed(X, G.shape, "X", G.dtype, G.device)
+    ws, nbytes = _space(workspace, orthogonalize_workspace_bytes(N, m, n), G.device, made)
+    ca, cb, cc = (float(c) for c in coeffs)
+    _launch("deeppcr_orthogonalize", stream, G.device,
+            (_ptr(G), _ptr(X), N, m, n, int(steps), ca, cb, cc, float(eps), dt, _ptr(ws), nbytes),
+            made)
+    return X
 
 
 def release_thread_state() -> None:

@@ -1,0 +1,140 @@
+"""Orthogonalised updates on the GPU against their float64 definition: types,
+shapes, ranges, and the gradients they are made for.
+
+Bounds.  A product of operands that carry 22 bits or more, accumulated in
+float32, errs by at most (2^-20 + K 2^-24) sqrt(k) of the operands' spectral
+sizes in norm for a k x K times K x r product; with A, A A and B X and the
+coefficients (3.4445 + 4.775 + 2.0315 = 10.3 of them, the gain of one step in
+size) a step adds at most 10.3 times three of these, and every later step
+magnifies it by at most its slope; over all steps that is `gain` times for the
+first and less for the others, 1.5 gain in all (a geometric sum with ratio
+1 / 3.4445).  So |X - ref|_2 <= 31 * 1.5 gain (2^-20 + K 2^-24) as the worst
+case.  Rounding errors of a product are random in sign; their sum over K
+products grows as its root, and a random matrix of entrywise errors e has
+spectral norm 2 sqrt(r) e instead of r e, which leaves
+
+    max |X - ref| <= gain (2^-20 + sqrt(K) 2^-24) max |ref|
+
+for each entry.  An output's rounding adds half a step of its type.
+"""
+import numpy as np
+import pytest
+
+import oracle
+from oracle import ortho_oracle as oo
+from paper_2309_16318_amd import deeppcr, synth
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+SHAPES = [(1, 1, 1), (3, 1, 5), (2, 5, 1), (4, 2, 2), (5, 16, 16), (3, 17, 17), (7, 32, 32),
+          (2, 31, 33), (3, 64, 64), (2, 40, 64), (2, 100, 100), (3, 128, 128), (2, 128, 16),
+          (2, 16, 128), (2, 129, 129), (1, 96, 200), (2, 200, 96), (1, 256, 256), (1, 1, 300),
+          (1, 333, 130), (1, 520, 264), (1, 130, 1025)]
+
+
+@pytest.fixture(scope="module")
+def dev():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return torch.device("cuda:0")
+
+
+def cpu(t):
+    return t.detach().double().cpu().numpy()
+
+
+def check(got, ref, dtype, steps=5, coeffs=oo.COEFFS):
+    got, half = cpu(got), torch.finfo(dtype).eps / 2
+    K = max(ref.shape[-2:])
+    top = np.max(np.abs(ref), axis=(-2, -1), keepdims=True)
+    e = max(1.0, oo.gain(steps, coeffs)) * (2.0 ** -20 + np.sqrt(K) * 2.0 ** -24)
+    assert np.all(np.isfinite(got)) and got.shape == ref.shape
+    tiny = torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+    bad = np.abs(got - ref) - (e * top + half * np.abs(ref) + tiny)
+    assert np.max(bad) <= 0, np.max(np.abs(got - ref) / top)
+
+
+def gradient(N, m, n, dtype, dev, seed=0):
+    gen = torch.Generator().manual_seed(seed + 13 * m + n)
+    return (torch.randn(N, m, n, generator=gen) * 0.02).to(dtype).to(dev)
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_shapes(dev, shape, kind):
+    G = gradient(*shape, TYPES[kind], dev)
+    check(deeppcr.deeppcr_orthogonalize(G), oo.orthogonalize(cpu(G)), TYPES[kind])
+
+
+@pytest.mark.parametrize("w", [12, 128, 160])
+def test_steps_and_coefficients(dev, w):
+    G = gradient(2, w, w, torch.float32, dev)
+    for steps, coeffs in ((0, oo.COEFFS), (1, oo.COEFFS), (2, (1.5, -0.5, 0.0)),
+                          (6, (1.875, -1.25, 0.375))):
+        got = deeppcr.deeppcr_orthogonalize(G, steps=steps, coeffs=coeffs)
+        check(got, oo.orthogonalize(cpu(G), steps, coeffs), torch.float32, steps, coeffs)
+    one = deeppcr.deeppcr_orthogonalize(G[1])
+    assert torch.equal(one, deeppcr.deeppcr_orthogonalize(G)[1])
+
+
+@pytest.mark.parametrize("w", [16, 64, 128, 150])
+def test_range(dev, w):
+    """Gradients far below and above the squares' float32 range, a zero
+    matrix, rank one, and non-finite ones that stay alone."""
+    G = gradient(8, w, w, torch.float32, dev)
+    G[0] *= 1e-37 / 0.02
+    G[1] = G[1] * 50 * 1e37
+    G[2] = 0
+    G[3] = torch.outer(G[3, 0], G[3, 1])
+    got = deeppcr.deeppcr_orthogonalize(G, eps=0.0)
+    ref = oo.orthogonalize(cpu(G), eps=0.0)
+    check(got, ref, torch.float32)
+    assert torch.all(got[2] == 0)
+    check(deeppcr.deeppcr_orthogonalize(G), oo.orthogonalize(cpu(G)), torch.float32)
+    G[4, 0, 0] = float("nan")
+    G[5, w - 1, 2] = float("inf")
+    bad = deeppcr.deeppcr_orthogonalize(G, eps=0.0)
+    keep = [0, 1, 2, 3, 6, 7]
+    assert torch.equal(bad[keep], got[keep])
+    assert torch.isnan(bad[4]).any() and torch.isnan(bad[5]).any()
+
+
+def test_in_place_and_same_bits(dev):
+    for shape in ((40, 24, 24), (3, 128, 128), (2, 300, 140)):
+        G = gradient(*shape, torch.float32, dev)
+        first = deeppcr.deeppcr_orthogonalize(G)
+        for _ in range(3):
+            assert torch.equal(first, deeppcr.deeppcr_orthogonalize(G))
+        X = G.clone()
+        assert deeppcr.deeppcr_orthogonalize(X, X=X) is X and torch.equal(X, first)
+
+
+def test_captured(dev):
+    for shape in ((5, 64, 64), (2, 200, 140)):
+        G = gradient(*shape, torch.bfloat16, dev)
+        X = torch.empty_like(G)
+        ws = torch.empty(deeppcr.orthogonalize_workspace_bytes(*shape), dtype=torch.uint8,
+                         device=dev)
+        deeppcr.deeppcr_orthogonalize(G, X=X, workspace=ws)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            deeppcr.deeppcr_orthogonalize(G, X=X, workspace=ws)
+        for _ in range(3):
+            G.copy_(torch.randn_like(G))
+            want = deeppcr.deeppcr_orthogonalize(G)
+            X.fill_(float("nan"))
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(X, want)
+
+
+def test_update_of_the_mlp_gradients(dev):
+    """dW of the library's own backward pass, every layer's update."""
+    B, L, w = 4, 12, 24
+    d = {k: torch.from_numpy(v).to(dev) for k, v in synth.mlp_inputs(B, L, w, seed=5).items()}
+    res = deeppcr.deeppcr_mlp_forward(d["W"], d["bias"], d["z0"])
+    dW = deeppcr.deeppcr_mlp_backward(d["W"], d["bias"], d["z0"], res.Z, d["G"])[2]
+    check(deeppcr.deeppcr_orthogonalize(dW, eps=0.0), oo.orthogonalize(cpu(dW), eps=0.0),
+          torch.float32)

@@ -151,3 +151,35 @@ def test_residual_norm_rejects_overlaps():
         for i in range(10):
             assert _nbwd(**{out: P[i]}) == E, (out, i)
     assert _nbwd(dx=P[11]) == E and _nbwd(ws=P[13]) == E
+
+
+def _ortho(G=P[0], X=P[1], N=3, m=20, n=30, steps=5, a=3.4445, b=-4.7750, c=2.0315, eps=1e-7,
+           dtype=0, ws=P[2], nws=BIG):
+    return deeppcr.lib().deeppcr_orthogonalize(G, X, N, m, n, steps, a, b, c, eps, dtype, ws, nws,
+                                               None)
+
+
+def test_orthogonalize_rejects_invalid_arguments():
+    f = deeppcr.orthogonalize_workspace_bytes
+    assert f(1, 1, 1) > 0 and f(2, 8192, 8192) > 0
+    for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1, 8193, 8), (1, 8, 8193), (-1, 2, 2)):
+        assert f(*bad) == 0
+    for k, p in (("G", P[0]), ("X", P[1]), ("ws", P[2])):
+        assert _ortho(**{k: None}) == E and _ortho(**{k: off(p, 8)}) == E
+    for bad in (dict(N=0), dict(m=0), dict(n=8193), dict(steps=-1), dict(dtype=3),
+                dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf"))):
+        assert _ortho(**bad) == E, bad
+    assert _ortho(X=off(P[0], 16)) == E and _ortho(ws=P[0]) == E and _ortho(ws=P[1]) == E
+    assert _ortho(nws=f(3, 20, 30) - 1) == deeppcr.EWORKSPACE
+
+
+def test_orthogonalize_rejects_polynomials_that_run_away():
+    W = deeppcr.EWORKSPACE        # a valid call with a short workspace
+    assert _ortho(nws=1) == W
+    for ok in ((1.5, -0.5, 0.0), (1.875, -1.25, 0.375), (3.4445, -4.7750, 2.0315), (0, 0, 0),
+               (1, 0, 0)):
+        assert _ortho(a=ok[0], b=ok[1], c=ok[2], steps=8, nws=1) == W, ok
+    for bad in ((100.0, 0, 0), (3.4445, 4.7750, 2.0315), (2.0, 0, 0), (1.5, -0.5, 30.0),
+                (float("nan"), 0, 0), (1, float("inf"), 0)):
+        assert _ortho(a=bad[0], b=bad[1], c=bad[2], steps=8, nws=1) == E, bad
+    assert _ortho(a=2.0, b=0, c=0, steps=2, nws=1) == W
