@@ -396,7 +396,7 @@ int deeppcr_seq_backward(const float* W, const float* bias, const float* z0, con
  * validation before any HIP call, no wait for the GPU, no overlap of an
  * output with another argument but where the text allows it, results that
  * are the same run to run.  Every launch is a kernel, so that each call can
- * sit in a captured graph.
+ * sit in a captured graph.  B w <= 2^31 - 64 and L <= 2^30.
  */
 enum { DEEPPCR_F32 = 0, DEEPPCR_BF16 = 1, DEEPPCR_F16 = 2 };
 enum {

@@ -1493,10 +1493,11 @@ namespace {
 
 int elem_size(int dtype) { return dtype == DEEPPCR_F32 ? 4 : 2; }
 
-// A launch has fewer than 2^32 threads, so the channels of a batch are limited.
+// A launch has fewer than 2^32 threads, so the channels of a batch are limited
+// (and their count, rounded up to whole waves, stays an int, as rows do).
 bool seq_ok(int B, int L, int w, int dtype) {
-    return B >= 1 && L >= 1 && w >= 1 && dtype >= DEEPPCR_F32 && dtype <= DEEPPCR_F16 &&
-           (double)B * w < 2147483648.0 && (double)B * L * w * 4.0 < 9.0e18;
+    return B >= 1 && L >= 1 && L <= (1 << 30) && w >= 1 && dtype >= DEEPPCR_F32 && dtype <= DEEPPCR_F16 &&
+           (double)B * w <= 2147483584.0 && (double)B * L * w * 4.0 < 9.0e18;
 }
 
 // A sequence with a row stride starts at any element.

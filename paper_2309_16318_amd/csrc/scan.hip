@@ -1,5 +1,19 @@
 // Gated linear recurrence: x_l = s_l x_{l-1} + r_l channel by channel, its
 // backward pass and the single row.
+//
+// A row maps the state x_in to s x_in + r, so a run of rows maps it to
+// A x_in + H with A the product of its multipliers and H its end from zero
+// (the diagonal form of the chunk maps P x_in + q of the block solves).  The
+// backward pass is the same recurrence on kap_l = s_l lam_l, the adjoint as
+// it leaves row l: kap_l = s_l kap_{l+1} + s_l g_l, walked from the last row.
+//
+// Bound by memory: every input is read once and every output written once.  A
+// workgroup of S waves takes a tile of S * R rows by 64 packs of V channels;
+// each thread loads its R rows of a pack at once into registers, folds them to
+// (A, H), gets its own x_in from the waves before it through LDS, and walks its
+// rows again from there, so a value takes its recurrence's order whatever the
+// tile.  Where the channels alone do not fill the chip a sequence's tiles run
+// at once: each publishes its (A, H) and takes its x_in from those before it.
 #include <type_traits>
 
 #include "elem.h"
@@ -8,65 +22,250 @@
 namespace deeppcr {
 namespace {
 
-// The multiplier s, the added part r, and c = 1 - s of one element.
+constexpr int R = 16;             // rows per thread
+constexpr int S = 8;              // most waves per workgroup
+constexpr int T = R * S;          // rows per tile
+constexpr int kSuper = 2 * S;     // tiles between two published states
+constexpr unsigned long long kEmpty = ~0ull;  // nothing published yet
+
+// The multiplier s, and the factor q of u, of one element.
 template <int GATE>
-__device__ __forceinline__ void gate_of(float a, float* s, float* c) {
+__device__ __forceinline__ void gate_of(float a, float* s, float* q) {
     if constexpr (GATE == 1) {
-        sigmoid_pair(a, s, c);
+        sigmoid_pair(a, s, q);
     } else {
         *s = a;
-        *c = 1.f;
+        *q = 1.f;
     }
 }
 
-template <int DT, int GATE>
-__global__ void __launch_bounds__(64) scan_walk(ScanArgs k) {
-    const long long f = (long long)blockIdx.x * 64 + threadIdx.x;
-    if (f >= (long long)k.B * k.w) return;
-    const int b = (int)(f / k.w), c = (int)(f % k.w);
-    const int n = k.lengths ? min(max(k.lengths[b], 0), k.L) : k.L;
-    const long long r0 = (long long)b * k.L;
-    float x = k.x0 ? k.x0[f] : 0.f;
-    float out[1];
-    for (int l = 0; l < n; ++l) {
-        float s, q;
-        gate_of<GATE>((float)pack_load<DT, 1>(k.a, (r0 + l) * k.lda + c).e[0], &s, &q);
-        x = fmaf(s, x, q * (float)pack_load<DT, 1>(k.u, (r0 + l) * k.ldu + c).e[0]);
-        out[0] = x;
-        pack_store<DT, 1>(k.out0, (r0 + l) * k.w + c, out);
-    }
-    out[0] = 0.f;
-    for (int l = n; l < k.L; ++l) pack_store<DT, 1>(k.out0, (r0 + l) * k.w + c, out);
-    if (k.last) k.last[f] = x;
+// A x + H; exactly H at x = 0, also where a long product A has overflowed (a
+// multiplier that is infinite or NaN itself makes H NaN).
+__device__ __forceinline__ float through(float A, float H, float x) {
+    return x == 0.f ? H : fmaf(A, x, H);
 }
 
-template <int DT, int GATE>
-__global__ void __launch_bounds__(64) scan_walk_bwd(ScanArgs k) {
-    const long long f = (long long)blockIdx.x * 64 + threadIdx.x;
-    if (f >= (long long)k.B * k.w) return;
-    const int b = (int)(f / k.w), c = (int)(f % k.w);
+// A pair as published: one 64-bit word, written and read whole, so that it
+// needs no flag beside it.  No pair has kEmpty's bits, because its NaNs are
+// made the canonical one.
+__device__ __forceinline__ void publish(unsigned long long* p, float A, float H) {
+    const unsigned nan = 0x7fc00000u;
+    const unsigned a = A == A ? __float_as_uint(A) : nan, h = H == H ? __float_as_uint(H) : nan;
+    __hip_atomic_store(p, (unsigned long long)h << 32 | a, __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+// Waits for a pair of a tile with a smaller ticket: that tile's workgroup is
+// running, and what it still waits for has a smaller ticket again.
+__device__ __forceinline__ void await(const unsigned long long* p, float* A, float* H) {
+    unsigned long long v;
+    while ((v = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == kEmpty)
+        __builtin_amdgcn_s_sleep(1);
+    *A = __uint_as_float((unsigned)v);
+    *H = __uint_as_float((unsigned)(v >> 32));
+}
+
+// How tiles talk: pairs [chunks, F, V] of every tile, states [supers, F, V]
+// behind every kSuper-th, and the next ticket.
+struct Board {
+    unsigned long long *pairs, *states;
+    unsigned* ticket;
+};
+
+__global__ void __launch_bounds__(256) scan_clear(unsigned long long* p, long long n,
+                                                  unsigned* ticket) {
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) p[i] = kEmpty;
+    if (i == 0) *ticket = 0;
+}
+
+// SPLIT: one tile per workgroup, by ticket, sequences' tiles side by side;
+// else a workgroup walks all tiles of its channels.
+template <int DT, int V, int GATE, bool BWD, bool SPLIT>
+__global__ void __launch_bounds__(64 * S, 4) scan_tile(ScanArgs k, Board bd, int groups, int chunks) {
+    __shared__ float sm[2][S][2][64 * V];   // (A, H) of the waves, two tiles in turn
+    __shared__ float lb[S][2][64 * V];      // of the tiles before, as each wave folded them
+    __shared__ float start[64 * V];
+    __shared__ unsigned ticket;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int waves = blockDim.x >> 6;
+    unsigned tile = blockIdx.x;
+    if constexpr (SPLIT) {
+        if (threadIdx.x == 0) ticket = atomicAdd(bd.ticket, 1u);
+        __syncthreads();
+        tile = __builtin_amdgcn_readfirstlane(ticket);
+    }
+    const int grp = SPLIT ? tile % groups : tile;
+    const int c0 = SPLIT ? tile / groups : 0, c1 = SPLIT ? c0 + 1 : chunks;
+    // pack f of all sequences' channels: sequence b, channels c .. c+V-1
+    const int cw = k.w / V, F = k.B * cw;
+    const int f = grp * 64 + lane;
+    const bool live = f < F;
+    const int fc = live ? f : F - 1;
+    const int b = fc / cw, c = (fc - b * cw) * V;
     const int n = k.lengths ? min(max(k.lengths[b], 0), k.L) : k.L;
     const long long r0 = (long long)b * k.L;
-    float out[1] = {0.f};
-    for (int l = n; l < k.L; ++l) {
-        pack_store<DT, 1>(k.out0, (r0 + l) * k.w + c, out);
-        pack_store<DT, 1>(k.out1, (r0 + l) * k.w + c, out);
+    const long long fv = (long long)fc * V;
+
+    float K[V];  // the state at the tile's start
+#pragma unroll
+    for (int v = 0; v < V; ++v) K[v] = 0.f;
+    const float* first = BWD ? k.g_last : k.x0;
+    if (first && c0 == 0 && (!SPLIT || wave == 0))
+#pragma unroll
+        for (int v = 0; v < V; ++v) K[v] = first[fv + v];
+
+    for (int ch = c0; ch < c1; ++ch) {
+        const int p0 = ch * T + wave * R;  // position in walking order
+        // row i of the thread, and whether this lane's sequence has it
+        auto row = [&](int i) { return BWD ? k.L - 1 - p0 - i : p0 + i; };
+        auto inside = [&](int i) { return BWD ? row(i) >= 0 : row(i) < k.L; };
+        auto has = [&](int i) { return row(i) < n && (!BWD || row(i) >= 0); };
+        Pack<DT, V> ra[R], ru[R], rx[R], rg[R];
+        {
+            // rows outside are read at the sequence's ends and not used
+            const bool some = (BWD ? row(R - 1) < n && row(0) >= 0 : row(0) < n);
+            if (__any(some)) {
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    const long long l = r0 + min(max(row(i), 0), k.L - 1);
+                    ra[i] = pack_load<DT, V>(k.a, l * k.lda + c);
+                    if (!BWD || GATE == 1) ru[i] = pack_load<DT, V>(k.u, l * k.ldu + c);
+                    if (BWD) {
+                        rg[i] = pack_load<DT, V>(k.g, l * k.ldg + c);
+                        const long long m = r0 + min(max(row(i) - 1, 0), k.L - 1);
+                        rx[i] = pack_load<DT, V>(k.x, m * k.w + c);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < R; ++i) ra[i] = ru[i] = rx[i] = rg[i] = Pack<DT, V>{};
+            }
+        }
+        float A[V], H[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v] = 1.f, H[v] = 0.f;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float s, q;
+                gate_of<GATE>((float)ra[i].e[v], &s, &q);
+                const float r = BWD ? s * (float)rg[i].e[v] : q * (float)ru[i].e[v];
+                if (has(i)) {
+                    A[v] *= s;
+                    H[v] = fmaf(s, H[v], r);
+                }
+            }
+        const int turn = ch & 1;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            sm[turn][wave][0][lane * V + v] = A[v];
+            sm[turn][wave][1][lane * V + v] = H[v];
+        }
+        __syncthreads();
+        if constexpr (SPLIT) {
+            const int sp = ch / kSuper, at = ch % kSuper;
+            float tA[V], tH[V];
+            if (wave == waves - 1) {  // the tile's own pair
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    tA[v] = 1.f;
+                    tH[v] = 0.f;
+                    for (int j = 0; j < waves; ++j) {
+                        const float a = sm[turn][j][0][lane * V + v];
+                        tH[v] = through(a, sm[turn][j][1][lane * V + v], tH[v]);
+                        tA[v] *= a;
+                    }
+                    if (live && ch > 0) publish(bd.pairs + ch * (long long)F * V + fv + v, tA[v], tH[v]);
+                }
+            }
+            // tiles 2 wave, 2 wave + 1 of those between the last published
+            // state and this tile
+#pragma unroll
+            for (int v = 0; v < V; ++v) A[v] = 1.f, H[v] = 0.f;
+            for (int j = 2 * wave; j < min(2 * wave + 2, at); ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    float a = 1.f, h = 0.f;
+                    if (live) await(bd.pairs + (sp * kSuper + j) * (long long)F * V + fv + v, &a, &h);
+                    H[v] = through(a, h, H[v]);
+                    A[v] *= a;
+                }
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                lb[wave][0][lane * V + v] = A[v];
+                lb[wave][1][lane * V + v] = H[v];
+            }
+            if (wave == 0)
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    float none;
+                    if (sp > 0 && live)
+                        await(bd.states + (sp - 1) * (long long)F * V + fv + v, &none, &K[v]);
+                    start[lane * V + v] = K[v];
+                }
+            __syncthreads();
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                K[v] = start[lane * V + v];
+                for (int j = 0; j < min(waves, (at + 1) / 2); ++j)
+                    K[v] = through(lb[j][0][lane * V + v], lb[j][1][lane * V + v], K[v]);
+                if (wave == waves - 1 && live) {
+                    const float end = through(tA[v], tH[v], K[v]);
+                    // the first tile's pair is its end, so that no other tile reads x0
+                    if (ch == 0) publish(bd.pairs + fv + v, 0.f, end);
+                    if (at == kSuper - 1)
+                        publish(bd.states + sp * (long long)F * V + fv + v, 0.f, end);
+                }
+            }
+        }
+        float h[V];  // the state at the thread's first row
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            h[v] = K[v];
+            for (int j = 0; j < waves; ++j) {
+                if (j == wave) h[v] = K[v];
+                if (!SPLIT || j < wave)
+                    K[v] = through(sm[turn][j][0][lane * V + v], sm[turn][j][1][lane * V + v], K[v]);
+            }
+            if (SPLIT) h[v] = K[v];
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            float o0[V], o1[V], xp[V];
+            if constexpr (BWD) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) xp[v] = (float)rx[i].e[v];
+                if (row(i) == 0)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) xp[v] = k.x0 ? k.x0[fv + v] : 0.f;
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float s, q;
+                gate_of<GATE>((float)ra[i].e[v], &s, &q);
+                if constexpr (BWD) {
+                    const float lam = h[v] + (float)rg[i].e[v];
+                    float d = xp[v];
+                    if (GATE == 1) d = (d - (float)ru[i].e[v]) * s * q;
+                    o0[v] = has(i) ? lam * d : 0.f;
+                    o1[v] = has(i) ? lam * q : 0.f;
+                    if (has(i)) h[v] = s * lam;
+                } else {
+                    if (has(i)) h[v] = fmaf(s, h[v], q * (float)ru[i].e[v]);
+                    o0[v] = has(i) ? h[v] : 0.f;
+                }
+            }
+            if (inside(i) && live) {
+                pack_store<DT, V>(k.out0, (r0 + row(i)) * k.w + c, o0);
+                if (BWD) pack_store<DT, V>(k.out1, (r0 + row(i)) * k.w + c, o1);
+            }
+        }
+        if (k.last && ch == chunks - 1 && wave == waves - 1 && live)
+#pragma unroll
+            for (int v = 0; v < V; ++v) k.last[fv + v] = h[v];
     }
-    float kap = k.g_last ? k.g_last[f] : 0.f;  // s_{l+1} lam_{l+1}
-    for (int l = n - 1; l >= 0; --l) {
-        float s, q;
-        gate_of<GATE>((float)pack_load<DT, 1>(k.a, (r0 + l) * k.lda + c).e[0], &s, &q);
-        const float lam = kap + (float)pack_load<DT, 1>(k.g, (r0 + l) * k.ldg + c).e[0];
-        float xp = l > 0 ? (float)pack_load<DT, 1>(k.x, (r0 + l - 1) * k.w + c).e[0]
-                         : (k.x0 ? k.x0[f] : 0.f);
-        if (GATE == 1) xp = (xp - (float)pack_load<DT, 1>(k.u, (r0 + l) * k.ldu + c).e[0]) * s * q;
-        out[0] = lam * xp;
-        pack_store<DT, 1>(k.out0, (r0 + l) * k.w + c, out);
-        out[0] = lam * q;
-        pack_store<DT, 1>(k.out1, (r0 + l) * k.w + c, out);
-        kap = s * lam;
-    }
-    if (k.last) k.last[f] = kap;
 }
 
 template <int DT, int GATE>
@@ -99,19 +298,56 @@ hipError_t by_type(int dtype, int gate, F&& f) {
     }
 }
 
+size_t up(size_t n) { return (n + 255) / 256 * 256; }
+long long chunks_of(int L) { return ((long long)L + T - 1) / T; }
+// Pairs and states, 8 bytes per channel each.
+size_t board_words(int B, int L, int w) {
+    const long long ch = chunks_of(L);
+    return (size_t)(ch + ch / kSuper) * B * w;
+}
+
+// Whether all rows may be read in packs of V.
+bool in_packs(const ScanArgs& k, int dtype, int V) {
+    const uintptr_t mask = (dtype == 0 ? 4 : 2) * V - 1;
+    auto ok = [&](const void* p, long long ld) { return !p || (((uintptr_t)p & mask) == 0 && ld % V == 0); };
+    return k.w % V == 0 && ok(k.a, k.lda) && ok(k.u, k.ldu) && ok(k.g, k.ldg);
+}
+
+template <int DT, int V, int GATE, bool BWD>
+hipError_t tiles(const ScanArgs& k, hipStream_t st) {
+    const long long F = (long long)k.B * (k.w / V), groups = (F + 63) / 64;
+    const long long chunks = chunks_of(k.L);
+    if (chunks > 1 && groups < 512 && groups * chunks < (1 << 22)) {
+        Board bd;
+        bd.ticket = (unsigned*)k.ws;
+        bd.pairs = (unsigned long long*)((char*)k.ws + 256);
+        bd.states = bd.pairs + chunks * F * V;
+        const long long n = (long long)board_words(k.B, k.L, k.w);
+        scan_clear<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(bd.pairs, n, bd.ticket);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        scan_tile<DT, V, GATE, BWD, true>
+            <<<(unsigned)(groups * chunks), 64 * S, 0, st>>>(k, bd, (int)groups, (int)chunks);
+    } else {
+        const int waves = k.L >= T ? S : (k.L + R - 1) / R;
+        scan_tile<DT, V, GATE, BWD, false>
+            <<<(unsigned)groups, 64 * waves, 0, st>>>(k, Board{}, (int)groups, (int)chunks);
+    }
+    return hipGetLastError();
+}
+
 }  // namespace
 
-size_t scan_workspace(int B, int L, int w) { return 256; }
+size_t scan_workspace(int B, int L, int w) { return 256 + up(board_words(B, L, w) * 8); }
 
 hipError_t launch_scan(bool bwd, const ScanArgs& k, int gate, int dtype, hipStream_t st) {
-    const unsigned grid = (unsigned)(((long long)k.B * k.w + 63) / 64);
     return by_type(dtype, gate, [&](auto dt, auto gt) {
         constexpr int DT = decltype(dt)::value, GATE = decltype(gt)::value;
-        if (bwd)
-            scan_walk_bwd<DT, GATE><<<grid, 64, 0, st>>>(k);
-        else
-            scan_walk<DT, GATE><<<grid, 64, 0, st>>>(k);
-        return hipGetLastError();
+        if constexpr (DT != 0) {
+            if (in_packs(k, dtype, 2))
+                return bwd ? tiles<DT, 2, GATE, true>(k, st) : tiles<DT, 2, GATE, false>(k, st);
+        }
+        return bwd ? tiles<DT, 1, GATE, true>(k, st) : tiles<DT, 1, GATE, false>(k, st);
     });
 }
 
