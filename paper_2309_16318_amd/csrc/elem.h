@@ -43,6 +43,44 @@ __device__ __forceinline__ void pack_store(void* base, long long i, const float 
     *reinterpret_cast<Pack<DT, V>*>(reinterpret_cast<elem_t<DT>*>(base) + i) = p;
 }
 
+// V consecutive elements as they lie in memory, in whole registers (two 16-bit
+// elements each): what a thread holds many of until it uses them.
+template <int DT, int V>
+struct Raw {
+    static constexpr int BYTES = (int)sizeof(elem_t<DT>) * V;
+    static constexpr int N = BYTES < 4 ? 1 : BYTES / 4;
+    unsigned word[N];
+    __device__ __forceinline__ void load(const void* base, long long i) {
+        const char* p = (const char*)base + i * (long long)sizeof(elem_t<DT>);
+        if constexpr (BYTES == 2) {
+            word[0] = *reinterpret_cast<const unsigned short*>(p);
+        } else {
+            struct alignas(BYTES) Words {
+                unsigned w[N];
+            };
+            const Words q = *reinterpret_cast<const Words*>(p);
+#pragma unroll
+            for (int j = 0; j < N; ++j) word[j] = q.w[j];
+        }
+    }
+    __device__ __forceinline__ float get(int v) const {
+        if constexpr (DT == 0) {
+            return __uint_as_float(word[v]);
+        } else if constexpr (DT == 1) {
+            return __uint_as_float(v & 1 ? word[v / 2] & 0xffff0000u : word[v / 2] << 16);
+        } else {
+            const unsigned short h = (unsigned short)(v & 1 ? word[v / 2] >> 16 : word[v / 2]);
+            return (float)__builtin_bit_cast(_Float16, h);
+        }
+    }
+    // From here on the compiler takes the words for new ones: what was
+    // computed from them before is not kept in registers for a second use.
+    __device__ __forceinline__ void renew() {
+#pragma unroll
+        for (int j = 0; j < N; ++j) asm volatile("" : "+v"(word[j]));
+    }
+};
+
 // s = sigmoid(a) and c = 1 - s, each to full relative precision: with
 // t = exp(-|a|) in (0, 1] neither overflows nor cancels.  NaN gives NaN.
 __device__ __forceinline__ void sigmoid_pair(float a, float* s, float* c) {

@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(64 * S, 4) scan_tile(ScanArgs k, Board bd, int
         auto row = [&](int i) { return BWD ? k.L - 1 - p0 - i : p0 + i; };
         auto inside = [&](int i) { return BWD ? row(i) >= 0 : row(i) < k.L; };
         auto has = [&](int i) { return row(i) < n && (!BWD || row(i) >= 0); };
-        Pack<DT, V> ra[R], ru[R], rx[R], rg[R];
+        Raw<DT, V> ra[R], ru[R], rx[R], rg[R];
         {
             // rows outside are read at the sequence's ends and not used
             const bool some = (BWD ? row(R - 1) < n && row(0) >= 0 : row(0) < n);
@@ -129,17 +129,17 @@ __global__ void __launch_bounds__(64 * S, 4) scan_tile(ScanArgs k, Board bd, int
 #pragma unroll
                 for (int i = 0; i < R; ++i) {
                     const long long l = r0 + min(max(row(i), 0), k.L - 1);
-                    ra[i] = pack_load<DT, V>(k.a, l * k.lda + c);
-                    if (!BWD || GATE == 1) ru[i] = pack_load<DT, V>(k.u, l * k.ldu + c);
+                    ra[i].load(k.a, l * k.lda + c);
+                    if (!BWD || GATE == 1) ru[i].load(k.u, l * k.ldu + c);
                     if (BWD) {
-                        rg[i] = pack_load<DT, V>(k.g, l * k.ldg + c);
+                        rg[i].load(k.g, l * k.ldg + c);
                         const long long m = r0 + min(max(row(i) - 1, 0), k.L - 1);
-                        rx[i] = pack_load<DT, V>(k.x, m * k.w + c);
+                        rx[i].load(k.x, m * k.w + c);
                     }
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < R; ++i) ra[i] = ru[i] = rx[i] = rg[i] = Pack<DT, V>{};
+                for (int i = 0; i < R; ++i) ra[i] = ru[i] = rx[i] = rg[i] = Raw<DT, V>{};
             }
         }
         float A[V], H[V];
@@ -150,8 +150,8 @@ __global__ void __launch_bounds__(64 * S, 4) scan_tile(ScanArgs k, Board bd, int
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 float s, q;
-                gate_of<GATE>((float)ra[i].e[v], &s, &q);
-                const float r = BWD ? s * (float)rg[i].e[v] : q * (float)ru[i].e[v];
+                gate_of<GATE>(ra[i].get(v), &s, &q);
+                const float r = BWD ? s * rg[i].get(v) : q * ru[i].get(v);
                 if (has(i)) {
                     A[v] *= s;
                     H[v] = fmaf(s, H[v], r);
@@ -233,10 +233,13 @@ __global__ void __launch_bounds__(64 * S, 4) scan_tile(ScanArgs k, Board bd, int
         }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
+            ra[i].renew();
+            if (BWD) rg[i].renew();
+            if (!BWD) ru[i].renew();
             float o0[V], o1[V], xp[V];
             if constexpr (BWD) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) xp[v] = (float)rx[i].e[v];
+                for (int v = 0; v < V; ++v) xp[v] = rx[i].get(v);
                 if (row(i) == 0)
 #pragma unroll
                     for (int v = 0; v < V; ++v) xp[v] = k.x0 ? k.x0[fv + v] : 0.f;
@@ -244,16 +247,16 @@ __global__ void __launch_bounds__(64 * S, 4) scan_tile(ScanArgs k, Board bd, int
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 float s, q;
-                gate_of<GATE>((float)ra[i].e[v], &s, &q);
+                gate_of<GATE>(ra[i].get(v), &s, &q);
                 if constexpr (BWD) {
-                    const float lam = h[v] + (float)rg[i].e[v];
+                    const float lam = h[v] + rg[i].get(v);
                     float d = xp[v];
-                    if (GATE == 1) d = (d - (float)ru[i].e[v]) * s * q;
+                    if (GATE == 1) d = (d - ru[i].get(v)) * s * q;
                     o0[v] = has(i) ? lam * d : 0.f;
                     o1[v] = has(i) ? lam * q : 0.f;
                     if (has(i)) h[v] = s * lam;
                 } else {
-                    if (has(i)) h[v] = fmaf(s, h[v], q * (float)ru[i].e[v]);
+                    if (has(i)) h[v] = fmaf(s, h[v], q * ru[i].get(v));
                     o0[v] = has(i) ? h[v] : 0.f;
                 }
             }
