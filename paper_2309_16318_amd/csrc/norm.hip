@@ -17,6 +17,7 @@ namespace deeppcr {
 namespace {
 
 constexpr int E = 8;          // columns per thread
+constexpr int kSumLanes = 64;  // threads that add up a column of partial sums
 constexpr int kSmallWG = 256;  // threads of a workgroup that holds several rows
 
 // The columns of thread t of a row's G threads: E in a row (VEC: w and the
@@ -37,6 +38,33 @@ struct Cols {
 #pragma unroll
             for (int j = 0; j < E; ++j)
                 f[j] = has(j) ? (float)pack_load<DT, 1>(row, at + c0 + j * step).e[0] : 0.f;
+        }
+    }
+    // the same, as it lies in memory (not VEC: an element per word)
+    struct Held {
+        Raw<DT, VEC ? E : 1> r[VEC ? 1 : E];
+        __device__ __forceinline__ float get(int j) const {
+            return VEC ? r[0].get(VEC ? j : 0) : r[VEC ? 0 : j].get(0);
+        }
+        __device__ __forceinline__ void renew() {
+#pragma unroll
+            for (auto& q : r) q.renew();
+        }
+    };
+    __device__ __forceinline__ void hold(const void* row, long long at, Held& h) const {
+        if constexpr (VEC) {
+            if (c0 < w)
+                h.r[0].load(row, at + c0);
+            else
+                h.r[0] = {};
+        } else {
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                if (has(j))
+                    h.r[j].load(row, at + c0 + j * step);
+                else
+                    h.r[j] = {};
+            }
         }
     }
     __device__ __forceinline__ void store(void* row, long long at, const float (&f)[E]) const {
@@ -119,8 +147,9 @@ struct Place {
     }
 };
 
-template <int DT, bool VEC, bool BIG>
-__global__ void __launch_bounds__(BIG ? 1024 : kSmallWG) norm_fwd(NormArgs k, int G) {
+template <int DT, bool VEC, int MAXT>
+__global__ void __launch_bounds__(MAXT ? MAXT : kSmallWG) norm_fwd(NormArgs k, int G) {
+    constexpr bool BIG = MAXT != 0;
     __shared__ float sm[2][16][1];
     const Place<BIG> me(G);
     const Cols<DT, VEC> cols(me.t, G, k.w);
@@ -180,8 +209,9 @@ __global__ void __launch_bounds__(BIG ? 1024 : kSmallWG) norm_fwd(NormArgs k, in
 //   dy = rstd_post (d c / n - n mean(d c)),  dz = d scale w_post n act'(z)
 // with sum(d c) = sum((dx_out + rstd_pre e) c) - rstd_pre mean(e m) sum(m c),
 // so that one reduction of three values serves both means.
-template <int DT, bool VEC, bool BIG>
-__global__ void __launch_bounds__(BIG ? 1024 : kSmallWG) norm_bwd(NormArgs k, int G, int parts) {
+template <int DT, bool VEC, int MAXT>
+__global__ void __launch_bounds__(MAXT ? MAXT : kSmallWG) norm_bwd(NormArgs k, int G, int parts) {
+    constexpr bool BIG = MAXT != 0;
     __shared__ float sm[2][16][3];
     __shared__ float tot[BIG ? 1 : kSmallWG * E];
     const Place<BIG> me(G);
@@ -200,59 +230,86 @@ __global__ void __launch_bounds__(BIG ? 1024 : kSmallWG) norm_bwd(NormArgs k, in
     const long long part = k.z_per_seq ? blockIdx.x % parts : blockIdx.x;
     const long long base = seq * k.L;
     const long long b0 = base + rows * part / parts, b1 = base + rows * (part + 1) / parts;
+    const bool row_gate = k.gate && !k.z_per_seq;
+    // A row as read.  The next row's loads are under way while one is worked on,
+    // where the registers allow it (16-bit elements, two to a register).
+    constexpr bool AHEAD = VEC && DT != 0 && MAXT <= 256;
+    struct Row {
+        typename Cols<DT, VEC>::Held x, y, z, d, h;
+        float rp, rq;
+    } now{}, next{};
+    auto fetch = [&](long long r0, Row& q) {
+        const long long r = r0 + me.sub < b1 ? r0 + me.sub : b1 - 1;
+        cols.hold(k.x, r * k.w, q.x);
+        if (k.y) cols.hold(k.y, r * k.ldy, q.y);
+        if (row_gate) cols.hold(k.z, r * k.ldz, q.z);
+        if (k.dx_out) cols.hold(k.dx_out, r * k.w, q.d);
+        if (k.dh) cols.hold(k.dh, r * k.w, q.h);
+        q.rp = k.w_post ? k.rstd_post[r] : 1.f;
+        q.rq = k.w_pre ? k.rstd_pre[r] : 0.f;
+    };
     float acc1[E] = {}, acc2[E] = {};
     float z[E] = {}, v[E], slope[E];
     if (k.gate && k.z_per_seq) cols.load(k.z, seq * k.ldz, z);
     gate_values(k.gate, z, v, slope);
+    if (AHEAD) fetch(b0, next);
     for (long long r0 = b0; r0 < b1; r0 += me.subs) {
         const bool live = r0 + me.sub < b1;
         const long long r = live ? r0 + me.sub : b1 - 1;
-        float x[E], y[E] = {}, d[E] = {}, dh[E] = {};
-        cols.load(k.x, r * k.w, x);
-        if (k.y) cols.load(k.y, r * k.ldy, y);
-        if (k.gate && !k.z_per_seq) {
-            cols.load(k.z, r * k.ldz, z);
+        if constexpr (AHEAD) {
+            now = next;
+            if (r0 + me.subs < b1) fetch(r0 + me.subs, next);
+        } else {
+            fetch(r0, now);
+        }
+        if (row_gate) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) z[j] = now.z.get(j);
             gate_values(k.gate, z, v, slope);
         }
-        if (k.dx_out) cols.load(k.dx_out, r * k.w, d);
-        if (k.dh) cols.load(k.dh, r * k.w, dh);
-        const float rp = k.w_post ? k.rstd_post[r] : 1.f;
-        const float rq = k.w_pre ? k.rstd_pre[r] : 0.f;
+        const float rp = now.rp, rq = now.rq;
+        // n, m and d + rq e of a column
+        auto terms = [&](int j, float* n, float* c, float* m, float* d) {
+            *n = now.y.get(j) * rp;
+            *c = kw[j] * v[j] * *n;
+            *m = (now.x.get(j) + *c) * rq;
+            *d = fmaf(rq * pre[j], now.h.get(j), now.d.get(j));
+        };
         float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-            y[j] *= rp;
-            const float c = kw[j] * v[j] * y[j];
-            if (k.y) x[j] += c;
-            x[j] *= rq;
-            const float e = dh[j] * pre[j];
-            d[j] = fmaf(rq, e, d[j]);
-            s[0] = fmaf(e, x[j], s[0]);
-            s[1] = fmaf(d[j], c, s[1]);
-            s[2] = fmaf(x[j], c, s[2]);
+            float n, c, m, d;
+            terms(j, &n, &c, &m, &d);
+            s[0] = fmaf(now.h.get(j) * pre[j], m, s[0]);
+            s[1] = fmaf(d, c, s[1]);
+            s[2] = fmaf(m, c, s[2]);
         }
         sum(s);
         const float m1 = rq * s[0] * inv;
         const float m2 = k.w_post ? (s[1] - m1 * s[2]) * inv : 0.f;
+        now.x.renew();
+        now.y.renew();
+        now.d.renew();
+        now.h.renew();
+        float od[E], oy[E], oz[E];
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-            d[j] = fmaf(-m1, x[j], d[j]);
-            if (live) acc2[j] = fmaf(dh[j], x[j], acc2[j]);
-        }
-        if (live) cols.store(k.dx, r * k.w, d);
-        if (k.y) {
-            float o[E];
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const float dn = d[j] * y[j];
-                if (live) acc1[j] += k.z_per_seq ? dn : dn * v[j];
-                o[j] = rp * fmaf(d[j], kw[j] * v[j], -m2 * y[j]);
-                z[j] = k.z_per_seq ? z[j] : dn * kw[j] * slope[j];
-            }
+            float n, c, m, d;
+            terms(j, &n, &c, &m, &d);
+            d = fmaf(-m1, m, d);
+            od[j] = d;
+            const float dn = d * n;
             if (live) {
-                cols.store(k.dy, r * k.w, o);
-                if (k.gate && !k.z_per_seq) cols.store(k.dz, r * k.w, z);
+                acc2[j] = fmaf(now.h.get(j), m, acc2[j]);
+                acc1[j] = fmaf(dn, k.z_per_seq ? 1.f : v[j], acc1[j]);
             }
+            oy[j] = rp * fmaf(d, kw[j] * v[j], -m2 * n);
+            oz[j] = dn * kw[j] * slope[j];
+        }
+        if (live) {
+            cols.store(k.dx, r * k.w, od);
+            if (k.y) cols.store(k.dy, r * k.w, oy);
+            if (row_gate) cols.store(k.dz, r * k.w, oz);
         }
     }
     // the workgroup's sums: over the rows it held at a time, in their order
@@ -281,19 +338,25 @@ __global__ void __launch_bounds__(BIG ? 1024 : kSmallWG) norm_bwd(NormArgs k, in
     finish(acc2, k.part2);
 }
 
-// Sums over n rows of one column by 16 threads, in a fixed order.
+// Sums over n rows of one column by LANES threads, in a fixed order.
+template <int LANES>
 __device__ __forceinline__ float column_sum(const float* p, long long n, int w, int c, int lane,
                                             float (*sm)[17]) {
-    float t = 0.f;
-    if (c < w)
-        for (long long i = lane; i < n; i += 16) t += p[i * w + c];
-    __syncthreads();
-    sm[lane][threadIdx.x & 15] = t;
-    __syncthreads();
-    t = 0.f;
+    float t[4] = {};
+    if (c < w) {
+        long long i = lane;
+        for (; i + 3 * LANES < n; i += 4 * LANES)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t += sm[i][threadIdx.x & 15];
-    return t;
+            for (int u = 0; u < 4; ++u) t[u] += p[(i + u * LANES) * w + c];
+        for (; i < n; i += LANES) t[0] += p[i * w + c];
+    }
+    __syncthreads();
+    sm[lane][threadIdx.x & 15] = (t[0] + t[1]) + (t[2] + t[3]);
+    __syncthreads();
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < LANES; ++i) s += sm[i][threadIdx.x & 15];
+    return s;
 }
 
 // One gate per sequence: a sequence's sums over its workgroups; dz from them,
@@ -304,8 +367,8 @@ __global__ void __launch_bounds__(256) norm_bwd_seq(NormArgs k, int parts, float
     __shared__ float sm[16][17];
     const int c = blockIdx.x * 16 + (threadIdx.x & 15), lane = threadIdx.x >> 4;
     const long long b = blockIdx.y;
-    const float t = column_sum(k.part1 + b * parts * k.w, parts, k.w, c, lane, sm);
-    const float u = k.part2 ? column_sum(k.part2 + b * parts * k.w, parts, k.w, c, lane, sm) : 0.f;
+    const float t = column_sum<16>(k.part1 + b * parts * k.w, parts, k.w, c, lane, sm);
+    const float u = k.part2 ? column_sum<16>(k.part2 + b * parts * k.w, parts, k.w, c, lane, sm) : 0.f;
     if (lane != 0 || c >= k.w) return;
     float z[E] = {(float)pack_load<DT, 1>(k.z, b * k.ldz + c).e[0]}, v[E], slope[E];
     gate_values(k.gate, z, v, slope);
@@ -317,19 +380,19 @@ __global__ void __launch_bounds__(256) norm_bwd_seq(NormArgs k, int parts, float
 }
 
 // The weights' gradients from n rows of partial sums.
-__global__ void __launch_bounds__(256) norm_bwd_sum(NormArgs k, const float* p1, const float* p2,
+__global__ void __launch_bounds__(16 * kSumLanes) norm_bwd_sum(NormArgs k, const float* p1, const float* p2,
                                                     long long n) {
-    __shared__ float sm[16][17];
+    __shared__ float sm[kSumLanes][17];
     const int c = blockIdx.x * 16 + (threadIdx.x & 15), lane = threadIdx.x >> 4;
     if (p1) {
-        const float t = column_sum(p1, n, k.w, c, lane, sm);
+        const float t = column_sum<kSumLanes>(p1, n, k.w, c, lane, sm);
         if (lane == 0 && c < k.w) {
             if (k.dscale) k.dscale[c] = t * (k.w_post ? k.w_post[c] : 1.f);
             if (k.dw_post) k.dw_post[c] = t * (k.scale ? k.scale[c] : 1.f);
         }
     }
     if (p2) {
-        const float t = column_sum(p2, n, k.w, c, lane, sm);
+        const float t = column_sum<kSumLanes>(p2, n, k.w, c, lane, sm);
         if (lane == 0 && c < k.w) k.dw_pre[c] = t;
     }
 }
@@ -357,14 +420,16 @@ int parts_of(const NormArgs& k) {
     return (int)(most < want ? most : want);
 }
 
+// f(DT, VEC, MAXT): MAXT = 0 several rows in a workgroup, else its most threads
+// (a row of 2048 columns or fewer leaves each thread more registers).
 template <class F>
-hipError_t by_kind(int dtype, bool vec, bool big, F&& f) {
-    using T = std::true_type;
-    using N = std::false_type;
-    auto g = [&](auto dt) {
-        return vec ? (big ? f(dt, T{}, T{}) : f(dt, T{}, N{}))
-                   : (big ? f(dt, N{}, T{}) : f(dt, N{}, N{}));
+hipError_t by_kind(int dtype, bool vec, int threads, F&& f) {
+    auto h = [&](auto dt, auto vc) {
+        if (threads <= 64) return f(dt, vc, std::integral_constant<int, 0>{});
+        if (threads <= 256) return f(dt, vc, std::integral_constant<int, 256>{});
+        return f(dt, vc, std::integral_constant<int, 1024>{});
     };
+    auto g = [&](auto dt) { return vec ? h(dt, std::true_type{}) : h(dt, std::false_type{}); };
     if (dtype == 0) return g(std::integral_constant<int, 0>{});
     if (dtype == 1) return g(std::integral_constant<int, 1>{});
     return g(std::integral_constant<int, 2>{});
@@ -397,7 +462,7 @@ hipError_t launch_norm_fwd(const NormArgs& k, int dtype, hipStream_t st) {
     const long long need = ((long long)k.B * k.L + subs - 1) / subs;
     const long long most = 256 * (2048 / threads);
     const unsigned grid = (unsigned)(need < most ? need : most);
-    return by_kind(dtype, packed(k, dtype), big, [&](auto dt, auto vec, auto bg) {
+    return by_kind(dtype, packed(k, dtype), G, [&](auto dt, auto vec, auto bg) {
         norm_fwd<decltype(dt)::value, decltype(vec)::value, decltype(bg)::value>
             <<<grid, threads, 0, st>>>(k, G);
         return hipGetLastError();
@@ -414,7 +479,7 @@ hipError_t launch_norm_bwd(const NormArgs& k0, int dtype, hipStream_t st) {
     float* ws = (float*)k.ws;
     if (want1 || k.z_per_seq) k.part1 = ws;
     if (want2) k.part2 = ws + groups * k.w;
-    hipError_t e = by_kind(dtype, packed(k, dtype), big, [&](auto dt, auto vec, auto bg) {
+    hipError_t e = by_kind(dtype, packed(k, dtype), G, [&](auto dt, auto vec, auto bg) {
         norm_bwd<decltype(dt)::value, decltype(vec)::value, decltype(bg)::value>
             <<<(unsigned)groups, big ? G : kSmallWG, 0, st>>>(k, G, parts);
         return hipGetLastError();
@@ -449,7 +514,7 @@ hipError_t launch_norm_bwd(const NormArgs& k0, int dtype, hipStream_t st) {
         p2 = want2 ? s2 : nullptr;
         n = k.B;
     }
-    if (p1 || p2) norm_bwd_sum<<<cols, 256, 0, st>>>(k, p1, p2, n);
+    if (p1 || p2) norm_bwd_sum<<<cols, 16 * kSumLanes, 0, st>>>(k, p1, p2, n);
     return hipGetLastError();
 }
 
