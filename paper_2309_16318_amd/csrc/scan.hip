@@ -22,10 +22,17 @@
 namespace deeppcr {
 namespace {
 
-constexpr int R = 16;             // rows per thread
-constexpr int S = 8;              // most waves per workgroup
-constexpr int T = R * S;          // rows per tile
-constexpr int kSuper = 2 * S;     // tiles between two published states
+// Tiles of 64 or 256 rows, packs of 4 and 1 or 4 earlier tiles per wave were
+// measured too: one sequence of 65536 rows of 1024 bfloat16 channels, forward
+// and backward, 320, 287, 413, 299 and 275 us against 263, 8 of 2048 x 2048 159,
+// 169, 200, 156 and 158 against 158, a prompt of 8192 x 2048 40, 42, 48, 40 and
+// 38 against 39.
+constexpr int R = 16;              // rows per thread
+constexpr int S = 8;               // most waves per workgroup
+constexpr int T = R * S;           // rows per tile
+constexpr int kBack = 2;           // earlier tiles that a wave folds
+constexpr int kSuper = kBack * S;  // tiles between two published states
+typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
 constexpr unsigned long long kEmpty = ~0ull;  // nothing published yet
 
 // The multiplier s, and the factor q of u, of one element.
@@ -54,28 +61,40 @@ __device__ __forceinline__ void publish(unsigned long long* p, float A, float H)
     __hip_atomic_store(p, (unsigned long long)h << 32 | a, __ATOMIC_RELAXED,
                        __HIP_MEMORY_SCOPE_AGENT);
 }
-// Waits for a pair of a tile with a smaller ticket: that tile's workgroup is
-// running, and what it still waits for has a smaller ticket again.
-__device__ __forceinline__ void await(const unsigned long long* p, float* A, float* H) {
-    unsigned long long v;
-    while ((v = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == kEmpty)
+__device__ __forceinline__ unsigned long long peek(const unsigned long long* p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// Waits for a word of a tile with a smaller ticket, given as it was at first:
+// that tile's workgroup is running, and what it still waits for has a smaller
+// ticket again.
+__device__ __forceinline__ void await(const unsigned long long* p, unsigned long long v, float* A,
+                                      float* H) {
+    while (v == kEmpty) {
         __builtin_amdgcn_s_sleep(1);
+        v = peek(p);
+    }
     *A = __uint_as_float((unsigned)v);
     *H = __uint_as_float((unsigned)(v >> 32));
 }
 
 // How tiles talk: pairs [chunks, F, V] of every tile, states [supers, F, V]
-// behind every kSuper-th, and the next ticket.
+// behind every kSuper-th, and the next ticket of each group of 64 packs.
+// (Tickets of all groups from one counter: 8 us of a prompt's 44, its atomics
+// being done one after the other.)
 struct Board {
     unsigned long long *pairs, *states;
-    unsigned* ticket;
+    unsigned* tickets;
 };
+constexpr int kApart = 32;       // words between two groups' tickets, a cache line
+constexpr int kMaxGroups = 512;  // as many as are worth splitting
 
 __global__ void __launch_bounds__(256) scan_clear(unsigned long long* p, long long n,
-                                                  unsigned* ticket) {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) p[i] = kEmpty;
-    if (i == 0) *ticket = 0;
+                                                  unsigned* tickets) {
+    // n is even: two words to a store
+    const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 2;
+    for (long long i = at; i < n; i += (long long)gridDim.x * 512)
+        __builtin_nontemporal_store(u64x2{kEmpty, kEmpty}, reinterpret_cast<u64x2*>(p + i));
+    if (at < 2 * kMaxGroups) tickets[at / 2 * kApart] = 0;
 }
 
 // SPLIT: one tile per workgroup, by ticket, sequences' tiles side by side;
@@ -89,14 +108,17 @@ __global__ void __launch_bounds__(64 * S, 4) scan_tile(ScanArgs k, Board bd, int
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6;
-    unsigned tile = blockIdx.x;
+    // A group's tiles in the order in which its workgroups get their tickets;
+    // the groups one further every round, so that no XCD (workgroups go to them
+    // in turn) reads the same columns, which lie in few channels of its L2.
+    const int grp = SPLIT ? (blockIdx.x + blockIdx.x / groups) % groups : blockIdx.x;
+    int c0 = 0;
     if constexpr (SPLIT) {
-        if (threadIdx.x == 0) ticket = atomicAdd(bd.ticket, 1u);
+        if (threadIdx.x == 0) ticket = atomicAdd(bd.tickets + grp * kApart, 1u);
         __syncthreads();
-        tile = __builtin_amdgcn_readfirstlane(ticket);
+        c0 = __builtin_amdgcn_readfirstlane(ticket);
     }
-    const int grp = SPLIT ? tile % groups : tile;
-    const int c0 = SPLIT ? tile / groups : 0, c1 = SPLIT ? c0 + 1 : chunks;
+    const int c1 = SPLIT ? c0 + 1 : chunks;
     // pack f of all sequences' channels: sequence b, channels c .. c+V-1
     const int cw = k.w / V, F = k.B * cw;
     const int f = grp * 64 + lane;
@@ -166,6 +188,7 @@ __global__ void __launch_bounds__(64 * S, 4) scan_tile(ScanArgs k, Board bd, int
         __syncthreads();
         if constexpr (SPLIT) {
             const int sp = ch / kSuper, at = ch % kSuper;
+            const long long tw = (long long)F * V;
             float tA[V], tH[V];
             if (wave == waves - 1) {  // the tile's own pair
 #pragma unroll
@@ -177,21 +200,34 @@ __global__ void __launch_bounds__(64 * S, 4) scan_tile(ScanArgs k, Board bd, int
                         tH[v] = through(a, sm[turn][j][1][lane * V + v], tH[v]);
                         tA[v] *= a;
                     }
-                    if (live && ch > 0) publish(bd.pairs + ch * (long long)F * V + fv + v, tA[v], tH[v]);
+                    if (live && ch > 0) publish(bd.pairs + ch * tw + fv + v, tA[v], tH[v]);
                 }
             }
-            // tiles 2 wave, 2 wave + 1 of those between the last published
-            // state and this tile
+            // kBack tiles per wave of those between the last published state
+            // and this tile, all asked for before one is waited for
+            const unsigned long long* board = bd.pairs + (sp * kSuper + kBack * wave) * tw + fv;
+            const int mine = min(max(at - kBack * wave, 0), kBack);
+            unsigned long long word[kBack][V], prev[V];
+#pragma unroll
+            for (int j = 0; j < kBack; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    if (live && j < mine) word[j][v] = peek(board + j * tw + v);
+            if (wave == 0 && sp > 0 && live)
+#pragma unroll
+                for (int v = 0; v < V; ++v) prev[v] = peek(bd.states + (sp - 1) * tw + fv + v);
 #pragma unroll
             for (int v = 0; v < V; ++v) A[v] = 1.f, H[v] = 0.f;
-            for (int j = 2 * wave; j < min(2 * wave + 2, at); ++j)
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    float a = 1.f, h = 0.f;
-                    if (live) await(bd.pairs + (sp * kSuper + j) * (long long)F * V + fv + v, &a, &h);
-                    H[v] = through(a, h, H[v]);
-                    A[v] *= a;
-                }
+            for (int j = 0; j < kBack; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    if (live && j < mine) {
+                        float a, h;
+                        await(board + j * tw + v, word[j][v], &a, &h);
+                        H[v] = through(a, h, H[v]);
+                        A[v] *= a;
+                    }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 lb[wave][0][lane * V + v] = A[v];
@@ -202,21 +238,21 @@ __global__ void __launch_bounds__(64 * S, 4) scan_tile(ScanArgs k, Board bd, int
                 for (int v = 0; v < V; ++v) {
                     float none;
                     if (sp > 0 && live)
-                        await(bd.states + (sp - 1) * (long long)F * V + fv + v, &none, &K[v]);
+                        await(bd.states + (sp - 1) * tw + fv + v, prev[v], &none, &K[v]);
                     start[lane * V + v] = K[v];
                 }
             __syncthreads();
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 K[v] = start[lane * V + v];
-                for (int j = 0; j < min(waves, (at + 1) / 2); ++j)
+                for (int j = 0; j < min(waves, (at + kBack - 1) / kBack); ++j)
                     K[v] = through(lb[j][0][lane * V + v], lb[j][1][lane * V + v], K[v]);
                 if (wave == waves - 1 && live) {
                     const float end = through(tA[v], tH[v], K[v]);
                     // the first tile's pair is its end, so that no other tile reads x0
                     if (ch == 0) publish(bd.pairs + fv + v, 0.f, end);
                     if (at == kSuper - 1)
-                        publish(bd.states + sp * (long long)F * V + fv + v, 0.f, end);
+                        publish(bd.states + sp * tw + fv + v, 0.f, end);
                 }
             }
         }
@@ -306,7 +342,7 @@ long long chunks_of(int L) { return ((long long)L + T - 1) / T; }
 // Pairs and states, 8 bytes per channel each.
 size_t board_words(int B, int L, int w) {
     const long long ch = chunks_of(L);
-    return (size_t)(ch + ch / kSuper) * B * w;
+    return ((size_t)(ch + ch / kSuper) * B * w + 1) / 2 * 2;
 }
 
 // Whether all rows may be read in packs of V.
@@ -320,13 +356,14 @@ template <int DT, int V, int GATE, bool BWD>
 hipError_t tiles(const ScanArgs& k, hipStream_t st) {
     const long long F = (long long)k.B * (k.w / V), groups = (F + 63) / 64;
     const long long chunks = chunks_of(k.L);
-    if (chunks > 1 && groups < 512 && groups * chunks < (1 << 22)) {
+    if (chunks > 1 && groups <= kMaxGroups && groups * chunks < (1 << 22)) {
         Board bd;
-        bd.ticket = (unsigned*)k.ws;
-        bd.pairs = (unsigned long long*)((char*)k.ws + 256);
+        bd.tickets = (unsigned*)k.ws;
+        bd.pairs = (unsigned long long*)((char*)k.ws + kMaxGroups * kApart * 4);
         bd.states = bd.pairs + chunks * F * V;
         const long long n = (long long)board_words(k.B, k.L, k.w);
-        scan_clear<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(bd.pairs, n, bd.ticket);
+        const long long wg = (n / 2 + 255) / 256;
+        scan_clear<<<(unsigned)(wg < 2 ? 2 : wg < 1024 ? wg : 1024), 256, 0, st>>>(bd.pairs, n, bd.tickets);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         scan_tile<DT, V, GATE, BWD, true>
@@ -341,7 +378,7 @@ hipError_t tiles(const ScanArgs& k, hipStream_t st) {
 
 }  // namespace
 
-size_t scan_workspace(int B, int L, int w) { return 256 + up(board_words(B, L, w) * 8); }
+size_t scan_workspace(int B, int L, int w) { return kMaxGroups * kApart * 4 + up(board_words(B, L, w) * 8); }
 
 hipError_t launch_scan(bool bwd, const ScanArgs& k, int gate, int dtype, hipStream_t st) {
     return by_type(dtype, gate, [&](auto dt, auto gt) {
