@@ -163,17 +163,38 @@ __global__ void __launch_bounds__(MAXT ? MAXT : kSmallWG) norm_fwd(NormArgs k, i
     const float inv = 1.f / (float)k.w;
     const long long rows = (long long)k.B * k.L;
     const long long step = (long long)gridDim.x * me.subs;
+    constexpr bool AHEAD = VEC && DT != 0;  // as in the backward pass
+    struct Row {
+        typename Cols<DT, VEC>::Held x, y, z;
+    } now{}, next{};
+    auto fetch = [&](long long r0, Row& q) {
+        const long long r = r0 + me.sub < rows ? r0 + me.sub : rows - 1;
+        cols.hold(k.x, r * k.w, q.x);
+        if (k.y) cols.hold(k.y, r * k.ldy, q.y);
+        if (k.gate) cols.hold(k.z, (k.z_per_seq ? r / k.L : r) * k.ldz, q.z);
+    };
+    const long long first = (long long)blockIdx.x * me.subs;
+    if (AHEAD && first < rows) fetch(first, next);
     // the same number of turns for all threads of the workgroup
-    for (long long r0 = (long long)blockIdx.x * me.subs; r0 < rows; r0 += step) {
+    for (long long r0 = first; r0 < rows; r0 += step) {
         const bool live = r0 + me.sub < rows;
         const long long r = live ? r0 + me.sub : rows - 1;
+        if constexpr (AHEAD) {
+            now = next;
+            if (r0 + step < rows) fetch(r0 + step, next);
+        } else {
+            fetch(r0, now);
+        }
         float x[E];
-        cols.load(k.x, r * k.w, x);
+#pragma unroll
+        for (int j = 0; j < E; ++j) x[j] = now.x.get(j);
         if (k.y) {
-            float y[E], v[E];
-            cols.load(k.y, r * k.ldy, y);
-            float z[E] = {};
-            if (k.gate) cols.load(k.z, (k.z_per_seq ? r / k.L : r) * k.ldz, z);
+            float y[E], z[E], v[E];
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                y[j] = now.y.get(j);
+                z[j] = now.z.get(j);
+            }
             gate_values(k.gate, z, v, nullptr);
             float rp = 1.f;
             if (k.w_post) {
