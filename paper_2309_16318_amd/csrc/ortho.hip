@@ -1,7 +1,23 @@
 // Orthogonalised update: X = G / (|G| + eps), then per step A = X X^T,
 // B = cb A + cc A A, X = ca X + B X on every matrix of a stack.  A matrix with
-// more rows than columns is worked on as its transpose.
+// more rows than columns is worked on as its transpose, X [k, r] with k <= r.
+//
+// Bound by the matrix cores.  A float32 value is carried by two float16 parts,
+// x 2^10 = hi + lo, 22 bits of it: singular values start at most at 1, and the
+// caller has made sure that no iterate or polynomial passes 15, so 2^10 x stays
+// in range.  A product is hi hi + hi lo + lo hi on the float16 matrix cores
+// with float32 accumulation; lo lo is below 2^-22 of it.  (The float32
+// instructions have a sixteenth of the float16 ones' rate, against a third.)
+// The iterates stay in these parts between the products.  A and A A are
+// symmetric: their tiles on and above the diagonal are computed and written
+// twice.
+//
+// A gradient far below eps makes a small X, which only its linear term moves
+// until it has grown.  It is held as Y = 2^e X with e from the norm that the
+// linear term gives it, so that its parts keep their bits:
+//   Y' = 2^(e'-e) (ca Y + (cb 2^-2e A + cc 2^-4e A A) Y),  A = Y Y^T.
 #include <algorithm>
+#include <type_traits>
 
 #include "elem.h"
 #include "internal.h"
@@ -9,125 +25,400 @@
 namespace deeppcr {
 namespace {
 
-constexpr int TS = 32;  // tile side
+typedef _Float16 h16;
+typedef h16 h16x8 __attribute__((ext_vector_type(8)));
+typedef h16 h16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-// One workgroup per matrix: X [k, r] from G [m, n] (transposed where m > n),
-// scaled to unit Frobenius norm by way of its largest element, so that no
-// square leaves the float32 range.
+constexpr float kScale = 1024.f, kUnscale = 1.f / 1024.f;  // 2^10
+
+__device__ __forceinline__ void split(float x, h16* hi, h16* lo) {
+    const float s = x * kScale;
+    *hi = (h16)s;
+    *lo = (h16)(s - (float)*hi);
+}
+__device__ __forceinline__ float join(h16 hi, h16 lo) {
+    return ((float)hi + (float)lo) * kUnscale;
+}
+
+// ------------------------------------------------------------------ the start
+constexpr int kParts = 64;  // most workgroups that share a matrix's norm
+
+// The largest size and the sum of squares against it of a part of a matrix,
+// so that no square leaves the float32 range: (top, sum) for workgroup
+// (part, matrix).
 template <int DT>
-__global__ void __launch_bounds__(256) ortho_scale(const void* G, float* X, int m, int n,
-                                                   float eps) {
-    __shared__ float sm[256];
-    const long long sz = (long long)m * n, base = blockIdx.x * sz;
-    float top = 0.f;
-    for (long long i = threadIdx.x; i < sz; i += 256)
-        top = fmaxf(top, fabsf((float)pack_load<DT, 1>(G, base + i).e[0]));
-    sm[threadIdx.x] = top;
-    __syncthreads();
-    for (int s = 128; s > 0; s /= 2) {
-        if (threadIdx.x < s) sm[threadIdx.x] = fmaxf(sm[threadIdx.x], sm[threadIdx.x + s]);
-        __syncthreads();
+__global__ void __launch_bounds__(256) ortho_norm(const void* G, float2* out, long long sz) {
+    __shared__ float sm[2][4];
+    const long long base = blockIdx.y * sz;
+    const long long b = sz * blockIdx.x / gridDim.x, e = sz * (blockIdx.x + 1) / gridDim.x;
+    float top = 0.f, bad = 0.f;
+    for (long long i = b + threadIdx.x; i < e; i += 256) {
+        const float g = fabsf((float)pack_load<DT, 1>(G, base + i).e[0]);
+        top = fmaxf(top, g);
+        bad += g * 0.f;  // NaN where g is not finite
     }
-    top = sm[0];
+    for (int m = 1; m < 64; m *= 2) {
+        top = fmaxf(top, __shfl_xor(top, m));
+        bad += __shfl_xor(bad, m);
+    }
+    if ((threadIdx.x & 63) == 0) sm[0][threadIdx.x >> 6] = top, sm[1][threadIdx.x >> 6] = bad;
+    __syncthreads();
+    top = fmaxf(fmaxf(sm[0][0], sm[0][1]), fmaxf(sm[0][2], sm[0][3]));
+    bad = (sm[1][0] + sm[1][1]) + (sm[1][2] + sm[1][3]);
     __syncthreads();
     float sum = 0.f;
-    for (long long i = threadIdx.x; i < sz; i += 256) {
-        const float g = (float)pack_load<DT, 1>(G, base + i).e[0];
-        const float v = g == 0.f ? 0.f : g / top;
-        sum = fmaf(v, v, sum);
-    }
-    sm[threadIdx.x] = sum;
+    if (top > 0.f)
+        for (long long i = b + threadIdx.x; i < e; i += 256) {
+            const float g = (float)pack_load<DT, 1>(G, base + i).e[0] / top;
+            sum = fmaf(g, g, sum);
+        }
+    for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
+    if ((threadIdx.x & 63) == 0) sm[0][threadIdx.x >> 6] = sum;
     __syncthreads();
-    for (int s = 128; s > 0; s /= 2) {
-        if (threadIdx.x < s) sm[threadIdx.x] += sm[threadIdx.x + s];
-        __syncthreads();
-    }
-    const float den = sqrtf(sm[0]) + eps / top;
-    for (long long i = threadIdx.x; i < sz; i += 256) {
-        const float g = (float)pack_load<DT, 1>(G, base + i).e[0];
-        const float v = g == 0.f && top == 0.f ? 0.f : g / top / den;
-        X[base + (m > n ? (i % n) * m + i / n : i)] = v;
-    }
+    if (threadIdx.x == 0)
+        out[blockIdx.y * gridDim.x + blockIdx.x] =
+            make_float2(top, (sm[0][0] + sm[0][1]) + (sm[0][2] + sm[0][3]) + bad);
 }
 
+// The factors by which a matrix becomes X: g / top * inv; its norm is
+// 2^-depth.
+struct Start {
+    float top, inv, depth;
+};
+__device__ __forceinline__ Start start_of(const float2* parts, int n, float eps) {
+    float top = 0.f, sum = 0.f;
+    for (int i = 0; i < n; ++i) top = fmaxf(top, parts[i].x);
+    for (int i = 0; i < n; ++i) {
+        const float f = parts[i].x > 0.f ? parts[i].x / top : 0.f;
+        sum = fmaf(parts[i].y, f * f, sum + (parts[i].y - parts[i].y));
+    }
+    // a zero matrix stays zero, whatever eps
+    if (top == 0.f) return {1.f, sum == sum ? 0.f : sum, 0.f};
+    const float norm = sqrtf(sum), den = norm + eps / top;
+    return {top, 1.f / den, log2f(den / norm)};
+}
+
+// e of step `step`, for a linear term that multiplies by 2^rate.
+__device__ __forceinline__ int shift_of(float depth, float rate, int step) {
+    const float e = floorf(depth - rate * (float)step);
+    return e > 0.f ? (int)fminf(e, 120.f) : 0;  // 0 where depth is NaN
+}
+
+// Planes of a stack: hi then lo of every matrix, [rows, cols] padded to whole
+// tiles with zeros.
+struct Planes {
+    h16* p;
+    long long sz;  // rows * cols
+    __device__ __forceinline__ h16* hi(long long z) const { return p + 2 * z * sz; }
+    __device__ __forceinline__ h16* lo(long long z) const { return p + (2 * z + 1) * sz; }
+};
+
+// X [kp, rp] and its transpose XT from G [m, n], 64 x 64 at a time.
 template <int DT>
-__global__ void __launch_bounds__(256) ortho_store(const float* X, void* out, int m, int n) {
-    const long long sz = (long long)m * n, base = blockIdx.x * sz;
-    for (long long i = threadIdx.x; i < sz; i += 256) {
-        const float v[1] = {X[base + (m > n ? (i % n) * m + i / n : i)]};
-        pack_store<DT, 1>(out, base + i, v);
-    }
-}
-
-// C [k, c] = alpha D + beta P Q (P [k, q]; Q [q, c], or stored [c, q]) for
-// matrix blockIdx.z.
-template <bool QT>
-__global__ void __launch_bounds__(256) ortho_product(const float* P, const float* Q, const float* D,
-                                                     float* C, int k, int q, int c, float alpha,
-                                                     float beta) {
-    __shared__ float p[TS][TS + 1], s[TS][TS + 1];
+__global__ void __launch_bounds__(256) ortho_start(const void* G, Planes X, Planes XT,
+                                                   const float2* parts, int nparts, float* depth,
+                                                   int m, int n, int kp, int rp, float eps) {
+    __shared__ float t[64][65];
     const long long z = blockIdx.z;
-    P += z * k * q;
-    Q += z * q * c;
-    C += z * k * c;
-    if (D) D += z * k * c;
-    const int i0 = blockIdx.y * TS, j0 = blockIdx.x * TS;
-    const int tx = threadIdx.x % TS, ty = threadIdx.x / TS;
-    float acc[4] = {};
-    for (int t0 = 0; t0 < q; t0 += TS) {
-        __syncthreads();
-        for (int y = ty; y < TS; y += 8) {
-            p[y][tx] = i0 + y < k && t0 + tx < q ? P[(long long)(i0 + y) * q + t0 + tx] : 0.f;
-            if (QT)
-                s[tx][y] = j0 + y < c && t0 + tx < q ? Q[(long long)(j0 + y) * q + t0 + tx] : 0.f;
-            else
-                s[y][tx] = t0 + y < q && j0 + tx < c ? Q[(long long)(t0 + y) * c + j0 + tx] : 0.f;
-        }
-        __syncthreads();
-        for (int t = 0; t < TS; ++t)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) acc[u] = fmaf(p[ty + 8 * u][t], s[t][tx], acc[u]);
+    const Start s = start_of(parts + z * nparts, nparts, eps);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) depth[z] = s.depth;
+    const float inv = ldexpf(s.inv, shift_of(s.depth, 0.f, 0));
+    const bool tall = m > n;
+    // rows i0.. and columns j0.. of G, padded like it
+    const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
+    const int cp = tall ? kp : rp, dp = tall ? rp : kp;  // padded columns and rows of G
+    Planes& P = tall ? XT : X;
+    Planes& Q = tall ? X : XT;
+    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
+        const int i = e / 64, j = e % 64;
+        float g = 0.f;
+        if (i0 + i < m && j0 + j < n)
+            g = (float)pack_load<DT, 1>(G, z * (long long)m * n + (long long)(i0 + i) * n + j0 + j).e[0];
+        g = g / s.top * inv;
+        if (i0 + i >= m || j0 + j >= n) g = 0.f;
+        t[i][j] = g;
+        h16 hi, lo;
+        split(g, &hi, &lo);
+        const long long at = (long long)(i0 + i) * cp + j0 + j;
+        P.hi(z)[at] = hi;
+        P.lo(z)[at] = lo;
     }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const int i = i0 + ty + 8 * u, j = j0 + tx;
-        if (i < k && j < c) {
-            const long long at = (long long)i * c + j;
-            C[at] = (D ? alpha * D[at] : 0.f) + beta * acc[u];
-        }
+    __syncthreads();
+    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
+        const int j = e / 64, i = e % 64;
+        h16 hi, lo;
+        split(t[i][j], &hi, &lo);
+        const long long at = (long long)(j0 + j) * dp + i0 + i;
+        Q.hi(z)[at] = hi;
+        Q.lo(z)[at] = lo;
     }
 }
 
-template <bool QT>
-hipError_t product(const float* P, const float* Q, const float* D, float* C, int N, int k, int q,
-                   int c, float alpha, float beta, hipStream_t st) {
-    const dim3 grid((c + TS - 1) / TS, (k + TS - 1) / TS, N);
-    ortho_product<QT><<<grid, 256, 0, st>>>(P, Q, D, C, k, q, c, alpha, beta);
+// With no steps: X itself.
+template <int DT>
+__global__ void __launch_bounds__(256) ortho_scaled(const void* G, void* X, const float2* parts,
+                                                    int nparts, long long sz, float eps) {
+    const long long z = blockIdx.y;
+    const Start s = start_of(parts + z * nparts, nparts, eps);
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < sz; i += gridDim.x * 256LL) {
+        const float v[1] = {(float)pack_load<DT, 1>(G, z * sz + i).e[0] / s.top * s.inv};
+        pack_store<DT, 1>(X, z * sz + i, v);
+    }
+}
+
+// --------------------------------------------------------------- the products
+enum { GRAM, POLY, APPLY };
+
+struct Product {
+    Planes P, Q;   // C[i, j] = sum_t P[i, t] Q[j, t]
+    Planes D, C;   // the own term and the result
+    Planes CT;     // APPLY: the result's transpose
+    void* out;     // last APPLY: X [m, n] instead
+    int rows, cols, K;  // padded
+    int m, n;
+    const float* depth;
+    float rate;
+    int step;
+    float own, times;   // own D + times P Q, before the shifts
+};
+
+// One tile of BM x BM per workgroup of 2 x 2 waves, in turn over the matrices
+// so that an XCD (workgroups go to the 8 of them in turn) works on few.
+template <int BM, int MODE, int OUT>
+__global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, long long all) {
+    constexpr int BK = 32, MT = BM / 64;
+    constexpr int LD = BM * 4 / 256;          // 16-byte chunks of a plane per thread
+    __shared__ h16 sm[2][2][2][BM * BK];      // buffer, operand, plane
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long per = (all + 7) / 8, id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= per || id >= all) return;
+    const long long z = id / tiles;
+    int bi, bj;
+    if constexpr (MODE == APPLY) {
+        const int nt = g.cols / BM;
+        bi = (int)(id % tiles) / nt;
+        bj = (int)(id % tiles) % nt;
+    } else {
+        // tiles bi <= bj, column by column
+        const int t = (int)(id % tiles);
+        bj = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+        while (bj * (bj + 1) / 2 > t) --bj;
+        while ((bj + 1) * (bj + 2) / 2 <= t) ++bj;
+        bi = t - bj * (bj + 1) / 2;
+    }
+    const h16* src[2][2] = {{g.P.hi(z), g.P.lo(z)}, {g.Q.hi(z), g.Q.lo(z)}};
+    const int row0[2] = {bi * BM, bj * BM};
+    h16x8 st[2][2][LD];
+    auto fetch = [&](int k0) {
+#pragma unroll
+        for (int o = 0; o < 2; ++o)
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int u = 0; u < LD; ++u) {
+                    const int q = threadIdx.x + 256 * u, row = q >> 2, c = q & 3;
+                    st[o][p][u] = *reinterpret_cast<const h16x8*>(
+                        src[o][p] + (long long)(row0[o] + row) * g.K + k0 + c * 8);
+                }
+    };
+    // chunk c of row `row` sits at c ^ (row / 4 mod 4): 16 rows that are read
+    // together then lie in different banks
+    auto place = [&](int b) {
+#pragma unroll
+        for (int o = 0; o < 2; ++o)
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int u = 0; u < LD; ++u) {
+                    const int q = threadIdx.x + 256 * u, row = q >> 2, c = q & 3;
+                    *reinterpret_cast<h16x8*>(&sm[b][o][p][row * BK + ((c ^ (row >> 2)) & 3) * 8]) =
+                        st[o][p][u];
+                }
+    };
+    const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BM / 2);
+    const int r32 = lane & 31, half = lane >> 5;
+    f32x16 acc[MT][MT] = {};
+    fetch(0);
+    place(0);
+    __syncthreads();
+    const int steps = g.K / BK;
+    for (int s = 0; s < steps; ++s) {
+        if (s + 1 < steps) fetch((s + 1) * BK);
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            h16x8 a[MT][2], b[MT][2];
+            const int c = kk * 2 + half;
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const int ra = wm + t * 32 + r32, rb = wn + t * 32 + r32;
+                    a[t][p] = *reinterpret_cast<const h16x8*>(
+                        &sm[s & 1][0][p][ra * BK + ((c ^ (ra >> 2)) & 3) * 8]);
+                    b[t][p] = *reinterpret_cast<const h16x8*>(
+                        &sm[s & 1][1][p][rb * BK + ((c ^ (rb >> 2)) & 3) * 8]);
+                }
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < MT; ++j) {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][1], b[j][0], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], b[j][1], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], b[j][0], acc[i][j], 0, 0, 0);
+                }
+        }
+        if (s + 1 < steps) place((s + 1) & 1);
+        __syncthreads();
+    }
+    // a lane holds column r32 of each 32 x 32 tile, rows 8 q + 4 half + 0 .. 3
+    float own = g.own, f = g.times * kUnscale * kUnscale;
+    int fin = 0;
+    if constexpr (MODE != GRAM) {
+        const int e = shift_of(g.depth[z], g.rate, g.step);
+        if constexpr (MODE == POLY) {
+            own = ldexpf(own, -2 * e);
+            f = ldexpf(f, -4 * e);
+        } else if constexpr (OUT >= 0) {
+            fin = -e;  // out of the shift; not in the factors, where it may be subnormal
+        } else {
+            const int d = shift_of(g.depth[z], g.rate, g.step + 1) - e;
+            own = ldexpf(own, d);
+            f = ldexpf(f, d);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int row = bi * BM + wm + i * 32 + 8 * q + 4 * half;
+                const int col = bj * BM + wn + j * 32 + r32;
+                h16x4 hi, lo;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = f * acc[i][j][4 * q + e];
+                    const long long at = (long long)(row + e) * g.cols + col;
+                    if (MODE != GRAM) v[e] = fmaf(own, join(g.D.hi(z)[at], g.D.lo(z)[at]), v[e]);
+                    h16 a, b;
+                    split(v[e], &a, &b);
+                    hi[e] = a;
+                    lo[e] = b;
+                }
+                if constexpr (OUT >= 0) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float one[1] = {ldexpf(v[e], fin)};
+                        const bool tall = g.m > g.n;
+                        const int r = tall ? col : row + e, c = tall ? row + e : col;
+                        if (r < g.m && c < g.n)
+                            pack_store<OUT < 0 ? 0 : OUT, 1>(
+                                g.out, (z * g.m + r) * (long long)g.n + c, one);
+                    }
+                } else {
+                    // as rows, and as columns: the transpose, or the tile below the diagonal
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const long long at = (long long)(row + e) * g.cols + col;
+                        g.C.hi(z)[at] = hi[e];
+                        g.C.lo(z)[at] = lo[e];
+                    }
+                    const Planes& T = MODE == APPLY ? g.CT : g.C;
+                    if (MODE == APPLY || bi != bj) {
+                        const long long at = (long long)col * g.rows + row;
+                        *reinterpret_cast<h16x4*>(T.hi(z) + at) = hi;
+                        *reinterpret_cast<h16x4*>(T.lo(z) + at) = lo;
+                    }
+                }
+            }
+}
+
+// ------------------------------------------------------------------- the plan
+// Sides are padded to whole tiles: 128 from 512 on (at most a quarter more),
+// 64 below.
+int padded(int n) { return n >= 512 ? (n + 127) / 128 * 128 : (n + 63) / 64 * 64; }
+
+struct Plan {
+    int k, r, kp, rp, parts;
+    long long some;  // matrices at a time
+    size_t xs, as;   // bytes of a matrix's X and A planes
+};
+Plan plan_of(int N, int m, int n) {
+    Plan p;
+    p.k = std::min(m, n);
+    p.r = std::max(m, n);
+    p.kp = padded(p.k);
+    p.rp = padded(p.r);
+    p.xs = (size_t)p.kp * p.rp * 4;
+    p.as = (size_t)p.kp * p.kp * 4;
+    p.parts = (int)std::min<long long>(kParts, ((long long)m * n + 16383) / 16384);
+    const size_t each = 3 * p.xs + 2 * p.as;
+    p.some = std::max<long long>(1, std::min<long long>({N, 32768, (long long)((1ull << 30) / each)}));
+    return p;
+}
+
+template <int MODE, int OUT>
+hipError_t product(const Product& g, int some, hipStream_t st) {
+    const int BM = g.rows % 128 == 0 && g.cols % 128 == 0 ? 128 : 64;
+    const long long ti = g.rows / BM, tj = g.cols / BM;
+    const int tiles = (int)(MODE == APPLY ? ti * tj : ti * (ti + 1) / 2);
+    const long long all = tiles * (long long)some;
+    const unsigned grid = (unsigned)((all + 7) / 8 * 8);
+    if (BM == 128)
+        ortho_product<128, MODE, OUT><<<grid, 256, 0, st>>>(g, tiles, all);
+    else
+        ortho_product<64, MODE, OUT><<<grid, 256, 0, st>>>(g, tiles, all);
     return hipGetLastError();
 }
 
-constexpr int kSome = 16384;  // matrices per launch (a grid's third axis ends at 65535)
-
 template <int DT>
 hipError_t run(const void* G, void* X, int N, int m, int n, int steps, float ca, float cb, float cc,
-               float eps, float* ws, hipStream_t st) {
-    const int k = std::min(m, n), r = std::max(m, n);
-    const long long sz = (long long)k * r, sq = (long long)k * k;
-    for (int at = 0; at < N; at += kSome) {
-        const int some = std::min(kSome, N - at);
-        float *x = ws, *y = x + some * sz, *A = y + some * sz, *B = A + some * sq;
-        const size_t es = sizeof(elem_t<DT>);
-        ortho_scale<DT><<<some, 256, 0, st>>>((const char*)G + at * sz * es, x, m, n, eps);
+               float eps, char* ws, hipStream_t st) {
+    const Plan p = plan_of(N, m, n);
+    const long long sz = (long long)m * n;
+    // a linear term that vanishes leaves nothing to hold on to
+    const float rate = ca == 0.f ? 0.f : log2f(fabsf(ca));
+    for (long long at = 0; at < N; at += p.some) {
+        const int some = (int)std::min<long long>(p.some, N - at);
+        const void* g = (const char*)G + at * sz * sizeof(elem_t<DT>);
+        void* out = (char*)X + at * sz * sizeof(elem_t<DT>);
+        float2* parts = (float2*)ws;
+        float* depth = (float*)(parts + p.some * kParts);
+        char* q = ws + (size_t)p.some * (kParts + 32) * sizeof(float2);
+        const long long xn = (long long)p.kp * p.rp, an = (long long)p.kp * p.kp;
+        const Planes x{(h16*)q, xn}, A{(h16*)(q + 3 * p.some * p.xs), an},
+            B{(h16*)(q + p.some * (3 * p.xs + p.as)), an};
+        Planes xt{(h16*)(q + p.some * p.xs), xn}, yt{(h16*)(q + 2 * p.some * p.xs), xn};
+        ortho_norm<DT><<<dim3(p.parts, some), 256, 0, st>>>(g, parts, sz);
         hipError_t e = hipGetLastError();
-        for (int s = 0; s < steps && e == hipSuccess; ++s) {
-            e = product<true>(x, x, nullptr, A, some, k, r, k, 0.f, 1.f, st);
-            if (e == hipSuccess) e = product<true>(A, A, A, B, some, k, k, k, cb, cc, st);
-            if (e == hipSuccess) e = product<false>(B, x, x, y, some, k, k, r, ca, 1.f, st);
-            std::swap(x, y);
-        }
         if (e != hipSuccess) return e;
-        ortho_store<DT><<<some, 256, 0, st>>>(x, (char*)X + at * sz * es, m, n);
+        if (steps == 0) {
+            const unsigned wg = (unsigned)std::min<long long>(256, (sz + 255) / 256);
+            ortho_scaled<DT><<<dim3(wg, some), 256, 0, st>>>(g, out, parts, p.parts, sz, eps);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            continue;
+        }
+        const int gr = m > n ? p.rp : p.kp, gc = m > n ? p.kp : p.rp;
+        ortho_start<DT><<<dim3(gc / 64, gr / 64, some), 256, 0, st>>>(g, x, xt, parts, p.parts,
+                                                                      depth, m, n, p.kp, p.rp, eps);
         e = hipGetLastError();
+        for (int s = 0; s < steps && e == hipSuccess; ++s) {
+            e = product<GRAM, -1>({x, x, {}, A, {}, nullptr, p.kp, p.kp, p.rp, m, n, depth,
+                                   rate, s, 0.f, 1.f},
+                                  some, st);
+            if (e == hipSuccess)
+                e = product<POLY, -1>({A, A, A, B, {}, nullptr, p.kp, p.kp, p.kp, m, n, depth,
+                                       rate, s, cb, cc},
+                                      some, st);
+            const Product last{B, xt, x, x, yt, out, p.kp, p.rp, p.kp, m, n, depth, rate, s, ca, 1.f};
+            if (e == hipSuccess)
+                e = s + 1 < steps ? product<APPLY, -1>(last, some, st)
+                                  : product<APPLY, DT>(last, some, st);
+            std::swap(xt, yt);
+        }
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -136,15 +427,15 @@ hipError_t run(const void* G, void* X, int N, int m, int n, int steps, float ca,
 }  // namespace
 
 size_t ortho_workspace(int N, int m, int n) {
-    const size_t k = std::min(m, n), r = std::max(m, n), some = std::min(N, kSome);
-    return some * (2 * k * r + 2 * k * k) * sizeof(float);
+    const Plan p = plan_of(N, m, n);
+    return (size_t)p.some * ((kParts + 32) * sizeof(float2) + 3 * p.xs + 2 * p.as);
 }
 
 hipError_t launch_ortho(const void* G, void* X, int N, int m, int n, int steps, float ca, float cb,
                         float cc, float eps, int dtype, void* ws, hipStream_t st) {
-    if (dtype == 0) return run<0>(G, X, N, m, n, steps, ca, cb, cc, eps, (float*)ws, st);
-    if (dtype == 1) return run<1>(G, X, N, m, n, steps, ca, cb, cc, eps, (float*)ws, st);
-    return run<2>(G, X, N, m, n, steps, ca, cb, cc, eps, (float*)ws, st);
+    if (dtype == 0) return run<0>(G, X, N, m, n, steps, ca, cb, cc, eps, (char*)ws, st);
+    if (dtype == 1) return run<1>(G, X, N, m, n, steps, ca, cb, cc, eps, (char*)ws, st);
+    return run<2>(G, X, N, m, n, steps, ca, cb, cc, eps, (char*)ws, st);
 }
 
 }  // namespace deeppcr
