@@ -335,6 +335,219 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
             }
 }
 
+// ----------------------------------------------------------- small matrices
+// A matrix of up to P x P (P = 32, 64, 128) stays in one workgroup for all
+// steps.  Wave v holds the columns 32 v .. 32 v + 31 of X in registers, as the
+// products leave them: column lane % 32, rows 8 q + 4 (lane / 32) + e of each 32
+// (q, e < 4).  Read as the right operand of a product these are the rows in the
+// order 0-3, 8-11 | 4-7, 12-15 of every 16; A and B, which meet them, have their
+// columns in LDS in that order, and their symmetry lets a lane write its column
+// as a row, four elements at once.  X goes to LDS by rows for the Gram product
+// only, then A, then B take its place.
+template <int P, int DT>
+__global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out, int m, int n,
+                                                        int steps, float ca, float cb, float cc,
+                                                        float eps, float rate) {
+    constexpr int NT = P / 32, PITCH = P + 8;  // a row's 16 bytes more spread the banks
+    __shared__ __attribute__((aligned(16))) h16 sm[2][P * PITCH];
+    __shared__ float red[2][NT];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r32 = lane & 31, half = lane >> 5;
+    const bool tall = m > n;
+    const int k = tall ? n : m, r = tall ? m : n;
+    const int rt = (k + 31) / 32;               // row tiles in use
+    const int ks = (k + 15) / 16, rs = (r + 15) / 16;
+    const int col = 32 * wave + r32;
+    const long long base = (long long)blockIdx.x * m * n;
+    auto row_of = [&](int t, int q, int e) { return 32 * t + 8 * q + 4 * half + e; };
+    auto at_of = [&](int row) { return base + (tall ? (long long)col * n + row : (long long)row * n + col); };
+
+    f32x16 acc[NT];
+    float top = 0.f, bad = 0.f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int row = row_of(t, i / 4, i % 4);
+            acc[t][i] = row < k && col < r ? (float)pack_load<DT, 1>(G, at_of(row)).e[0] : 0.f;
+            top = fmaxf(top, fabsf(acc[t][i]));
+            bad += acc[t][i] * 0.f;  // NaN where an element is not finite
+        }
+    for (int s = 1; s < 64; s *= 2) {
+        top = fmaxf(top, __shfl_xor(top, s));
+        bad += __shfl_xor(bad, s);
+    }
+    if (lane == 0) red[0][wave] = top, red[1][wave] = bad;
+    __syncthreads();
+    bad = 0.f;
+    for (int v = 0; v < NT; ++v) top = fmaxf(top, red[0][v]), bad += red[1][v];
+    __syncthreads();
+    float sum = 0.f;
+    if (top > 0.f)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                acc[t][i] /= top;
+                sum = fmaf(acc[t][i], acc[t][i], sum);
+            }
+    for (int s = 1; s < 64; s *= 2) sum += __shfl_xor(sum, s);
+    if (lane == 0) red[0][wave] = sum;
+    __syncthreads();
+    sum = bad;
+    for (int v = 0; v < NT; ++v) sum += red[0][v];
+    // a zero matrix stays zero, whatever eps; NaN stays NaN
+    float depth = 0.f, inv = sum == sum ? 0.f : sum;
+    if (top > 0.f) {
+        const float norm = sqrtf(sum), den = norm + eps / top;
+        inv = 1.f / den;
+        depth = log2f(den / norm);
+    }
+    inv = ldexpf(inv, shift_of(depth, 0.f, 0));
+    h16x8 xh[NT][2], xl[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            acc[t][i] *= inv;
+            h16 hi, lo;
+            split(acc[t][i], &hi, &lo);
+            xh[t][i / 8][i % 8] = hi;
+            xl[t][i / 8][i % 8] = lo;
+        }
+
+    // acc = sum over `count` steps of 16 of rows (32 t ..) of LDS against `right`
+    auto product = [&](int count, auto&& right) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[t] = f32x16{};
+#pragma unroll
+        for (int s = 0; s < P / 16; ++s) {
+            if (s >= count) break;
+            h16x8 b[2], a[NT][2];
+            right(s, b);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                if (t < rt)
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+                        a[t][p] = *reinterpret_cast<const h16x8*>(
+                            &sm[p][(32 * t + r32) * PITCH + 16 * s + 8 * half]);
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    if (t < rt)
+                        acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                            a[t][p == 0], b[p == 1], acc[t], 0, 0, 0);
+        }
+    };
+    // the wave's 32 rows of LDS as the right operand
+    auto own_rows = [&](int s, h16x8 (&b)[2]) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+            b[p] = *reinterpret_cast<const h16x8*>(&sm[p][col * PITCH + 16 * s + 8 * half]);
+    };
+    // rows 8 q + 4 half + 0 .. 3 of tile t of the lane's column, by symmetry
+    // columns of its row
+    auto run_of = [&](int t, int q) {
+        return col * PITCH + 32 * t + 16 * (q >> 1) + 4 * (2 * half + (q & 1));
+    };
+    const float f = kUnscale * kUnscale;
+    for (int s = 0; s < steps; ++s) {
+        const int e = shift_of(depth, rate, s);
+        const bool square = 32 * wave < k, wide = 32 * wave < r;
+        if (s > 0) __syncthreads();  // B has been read
+        if (wide)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                if (t < rt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int at = row_of(t, i / 4, i % 4) * PITCH + col;
+                        sm[0][at] = xh[t][i / 8][i % 8];
+                        sm[1][at] = xl[t][i / 8][i % 8];
+                    }
+        __syncthreads();
+        if (square) product(rs, own_rows);
+        __syncthreads();
+        auto put = [&](float times) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                if (t < rt)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        h16x4 hi, lo;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            h16 a, b;
+                            split(times * acc[t][4 * q + i], &a, &b);
+                            hi[i] = a;
+                            lo[i] = b;
+                        }
+                        *reinterpret_cast<h16x4*>(&sm[0][run_of(t, q)]) = hi;
+                        *reinterpret_cast<h16x4*>(&sm[1][run_of(t, q)]) = lo;
+                    }
+        };
+        if (square) put(f);  // A
+        __syncthreads();
+        if (square) {
+            product(ks, own_rows);
+            const float own = ldexpf(cb, -2 * e), times = ldexpf(cc * f, -4 * e);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                if (t < rt)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const h16x4 hi = *reinterpret_cast<const h16x4*>(&sm[0][run_of(t, q)]);
+                        const h16x4 lo = *reinterpret_cast<const h16x4*>(&sm[1][run_of(t, q)]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            acc[t][4 * q + i] =
+                                fmaf(own, join(hi[i], lo[i]), times * acc[t][4 * q + i]);
+                    }
+        }
+        __syncthreads();
+        if (square) put(1.f);  // B
+        __syncthreads();
+        if (!wide) continue;
+        product(ks, [&](int c, h16x8 (&b)[2]) {
+            b[0] = xh[c / 2][c % 2];
+            b[1] = xl[c / 2][c % 2];
+        });
+        const bool last = s + 1 == steps;
+        const int d = last ? 0 : shift_of(depth, rate, s + 1) - e;
+        const float own = ldexpf(ca, d), times = ldexpf(f, d);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float v = fmaf(own, join(xh[t][i / 8][i % 8], xl[t][i / 8][i % 8]),
+                                     times * acc[t][i]);
+                acc[t][i] = ldexpf(v, last ? -e : 0);
+                h16 hi, lo;
+                split(v, &hi, &lo);
+                xh[t][i / 8][i % 8] = hi;
+                xl[t][i / 8][i % 8] = lo;
+            }
+    }
+    if (steps == 0) {
+        const int e = shift_of(depth, 0.f, 0);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[t][i] = ldexpf(acc[t][i], -e);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int row = row_of(t, i / 4, i % 4);
+            const float v[1] = {acc[t][i]};
+            if (row < k && col < r) pack_store<DT, 1>(out, at_of(row), v);
+        }
+}
+
 // ------------------------------------------------------------------- the plan
 // Sides are padded to whole tiles: 128 from 512 on (at most a quarter more),
 // 64 below.
@@ -373,9 +586,36 @@ hipError_t product(const Product& g, int some, hipStream_t st) {
     return hipGetLastError();
 }
 
+// Sides up to 128.
+bool small_side(int m, int n) { return std::max(m, n) <= 128; }
+
+template <int DT>
+hipError_t run_small(const void* G, void* X, int N, int m, int n, int steps, float ca, float cb,
+                     float cc, float eps, hipStream_t st) {
+    const int side = std::max(m, n);
+    const float rate = ca == 0.f ? 0.f : log2f(fabsf(ca));
+    const long long sz = (long long)m * n * sizeof(elem_t<DT>);
+    // a launch has fewer than 2^32 threads
+    for (long long at = 0; at < N; at += 1 << 23) {
+        const unsigned some = (unsigned)std::min<long long>(1 << 23, N - at);
+        const void* g = (const char*)G + at * sz;
+        void* x = (char*)X + at * sz;
+        if (side <= 32)
+            ortho_small<32, DT><<<some, 64, 0, st>>>(g, x, m, n, steps, ca, cb, cc, eps, rate);
+        else if (side <= 64)
+            ortho_small<64, DT><<<some, 128, 0, st>>>(g, x, m, n, steps, ca, cb, cc, eps, rate);
+        else
+            ortho_small<128, DT><<<some, 256, 0, st>>>(g, x, m, n, steps, ca, cb, cc, eps, rate);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 template <int DT>
 hipError_t run(const void* G, void* X, int N, int m, int n, int steps, float ca, float cb, float cc,
                float eps, char* ws, hipStream_t st) {
+    if (small_side(m, n)) return run_small<DT>(G, X, N, m, n, steps, ca, cb, cc, eps, st);
     const Plan p = plan_of(N, m, n);
     const long long sz = (long long)m * n;
     // a linear term that vanishes leaves nothing to hold on to
@@ -427,6 +667,7 @@ hipError_t run(const void* G, void* X, int N, int m, int n, int steps, float ca,
 }  // namespace
 
 size_t ortho_workspace(int N, int m, int n) {
+    if (small_side(m, n)) return 256;
     const Plan p = plan_of(N, m, n);
     return (size_t)p.some * ((kParts + 32) * sizeof(float2) + 3 * p.xs + 2 * p.as);
 }
