@@ -43,60 +43,82 @@ __device__ __forceinline__ float join(h16 hi, h16 lo) {
 
 // ------------------------------------------------------------------ the start
 constexpr int kParts = 64;  // most workgroups that share a matrix's norm
+// Squares are summed in units of 2^160, 1 and 2^-160; to the next larger unit:
+__device__ __forceinline__ float next_unit(float sum) { return sum * 0x1p-80f * 0x1p-80f; }
 
-// The largest size and the sum of squares against it of a part of a matrix,
-// so that no square leaves the float32 range: (top, sum) for workgroup
-// (part, matrix).
+// Sums of squares of the large, ordinary and small elements of a part of a
+// matrix, so that no square leaves the float32 range.
 template <int DT>
-__global__ void __launch_bounds__(256) ortho_norm(const void* G, float2* out, long long sz) {
-    __shared__ float sm[2][4];
+__global__ void __launch_bounds__(256) ortho_norm(const void* G, float4* out, long long sz) {
+    __shared__ float sm[3][4];
+    constexpr int V = 16 / sizeof(elem_t<DT>);
     const long long base = blockIdx.y * sz;
-    const long long b = sz * blockIdx.x / gridDim.x, e = sz * (blockIdx.x + 1) / gridDim.x;
-    float top = 0.f, bad = 0.f;
-    for (long long i = b + threadIdx.x; i < e; i += 256) {
-        const float g = fabsf((float)pack_load<DT, 1>(G, base + i).e[0]);
-        top = fmaxf(top, g);
-        bad += g * 0.f;  // NaN where g is not finite
+    // whole packs where the matrices start on 16 bytes, else single elements
+    const bool packs = sz % V == 0;
+    const long long n = packs ? sz / V : sz;
+    const long long b = n * blockIdx.x / gridDim.x, e = n * (blockIdx.x + 1) / gridDim.x;
+    float big = 0.f, mid = 0.f, tiny = 0.f;
+    auto add = [&](float g) {
+        const float a = fabsf(g);
+        const bool l = a > 0x1p60f, s = a < 0x1p-60f;
+        const float x = l ? g * 0x1p-80f : s ? g * 0x1p80f : g;  // NaN is ordinary
+        if (l) big = fmaf(x, x, big);
+        if (s) tiny = fmaf(x, x, tiny);
+        if (!l && !s) mid = fmaf(x, x, mid);
+    };
+    if (packs) {
+#pragma unroll 4
+        for (long long i = b + threadIdx.x; i < e; i += 256) {
+            const Pack<DT, V> p = pack_load<DT, V>(G, base + i * V);
+#pragma unroll
+            for (int v = 0; v < V; ++v) add((float)p.e[v]);
+        }
+    } else {
+        for (long long i = b + threadIdx.x; i < e; i += 256)
+            add((float)pack_load<DT, 1>(G, base + i).e[0]);
     }
     for (int m = 1; m < 64; m *= 2) {
-        top = fmaxf(top, __shfl_xor(top, m));
-        bad += __shfl_xor(bad, m);
+        big += __shfl_xor(big, m);
+        mid += __shfl_xor(mid, m);
+        tiny += __shfl_xor(tiny, m);
     }
-    if ((threadIdx.x & 63) == 0) sm[0][threadIdx.x >> 6] = top, sm[1][threadIdx.x >> 6] = bad;
+    if ((threadIdx.x & 63) == 0) {
+        sm[0][threadIdx.x >> 6] = big;
+        sm[1][threadIdx.x >> 6] = mid;
+        sm[2][threadIdx.x >> 6] = tiny;
+    }
     __syncthreads();
-    top = fmaxf(fmaxf(sm[0][0], sm[0][1]), fmaxf(sm[0][2], sm[0][3]));
-    bad = (sm[1][0] + sm[1][1]) + (sm[1][2] + sm[1][3]);
-    __syncthreads();
-    float sum = 0.f;
-    if (top > 0.f)
-        for (long long i = b + threadIdx.x; i < e; i += 256) {
-            const float g = (float)pack_load<DT, 1>(G, base + i).e[0] / top;
-            sum = fmaf(g, g, sum);
-        }
-    for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
-    if ((threadIdx.x & 63) == 0) sm[0][threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0)
-        out[blockIdx.y * gridDim.x + blockIdx.x] =
-            make_float2(top, (sm[0][0] + sm[0][1]) + (sm[0][2] + sm[0][3]) + bad);
+    if (threadIdx.x == 0) {
+        auto all = [&](int i) { return (sm[i][0] + sm[i][1]) + (sm[i][2] + sm[i][3]); };
+        out[blockIdx.y * gridDim.x + blockIdx.x] = make_float4(all(0), all(1), all(2), 0.f);
+    }
 }
 
-// The factors by which a matrix becomes X: g / top * inv; its norm is
+// The factors by which a matrix becomes X: g * unit * inv; its norm is
 // 2^-depth.
 struct Start {
-    float top, inv, depth;
+    float unit, inv, depth;
 };
-__device__ __forceinline__ Start start_of(const float2* parts, int n, float eps) {
-    float top = 0.f, sum = 0.f;
-    for (int i = 0; i < n; ++i) top = fmaxf(top, parts[i].x);
+__device__ __forceinline__ Start start_of(const float4* parts, int n, float eps) {
+    float big = 0.f, mid = 0.f, tiny = 0.f;
     for (int i = 0; i < n; ++i) {
-        const float f = parts[i].x > 0.f ? parts[i].x / top : 0.f;
-        sum = fmaf(parts[i].y, f * f, sum + (parts[i].y - parts[i].y));
+        big += parts[i].x;
+        mid += parts[i].y;
+        tiny += parts[i].z;
     }
-    // a zero matrix stays zero, whatever eps
-    if (top == 0.f) return {1.f, sum == sum ? 0.f : sum, 0.f};
-    const float norm = sqrtf(sum), den = norm + eps / top;
-    return {top, 1.f / den, log2f(den / norm)};
+    // the largest elements' unit; two units below there is nothing beside them
+    float unit = 1.f, sum = mid + next_unit(tiny);
+    if (big > 0.f) {
+        unit = 0x1p-80f;
+        sum = big + next_unit(mid);
+    } else if (mid == 0.f) {
+        unit = 0x1p80f;
+        sum = tiny;
+    }
+    // a zero matrix stays zero, whatever eps; a NaN makes all of it NaN
+    if (sum == 0.f) return {1.f, 0.f, 0.f};
+    const float norm = sqrtf(sum), den = norm + eps * unit;
+    return {unit, 1.f / den, log2f(den / norm)};
 }
 
 // e of step `step`, for a linear term that multiplies by 2^rate.
@@ -105,20 +127,25 @@ __device__ __forceinline__ int shift_of(float depth, float rate, int step) {
     return e > 0.f ? (int)fminf(e, 120.f) : 0;  // 0 where depth is NaN
 }
 
-// Planes of a stack: hi then lo of every matrix, [rows, cols] padded to whole
-// tiles with zeros.
-struct Planes {
+// The parts of a stack of matrices [rows, cols], padded to whole tiles with
+// zeros, in panels of 32 columns: a row of a panel is 32 hi and 32 lo, one cache
+// line, and the rows of a panel follow each other, so that a tile's share of a
+// step is one run of memory.
+struct Panels {
     h16* p;
     long long sz;  // rows * cols
-    __device__ __forceinline__ h16* hi(long long z) const { return p + 2 * z * sz; }
-    __device__ __forceinline__ h16* lo(long long z) const { return p + (2 * z + 1) * sz; }
+    int rows;
+    __device__ __forceinline__ h16* at(long long z, int row, int col) const {
+        return p + 2 * z * sz + ((long long)(col >> 5) * rows + row) * 64 + (col & 31);
+    }
 };
+constexpr int kLo = 32;  // from hi to lo
 
 // X [kp, rp] and its transpose XT from G [m, n], 64 x 64 at a time.
 template <int DT>
-__global__ void __launch_bounds__(256) ortho_start(const void* G, Planes X, Planes XT,
-                                                   const float2* parts, int nparts, float* depth,
-                                                   int m, int n, int kp, int rp, float eps) {
+__global__ void __launch_bounds__(256) ortho_start(const void* G, Panels X, Panels XT,
+                                                   const float4* parts, int nparts, float* depth,
+                                                   int m, int n, float eps) {
     __shared__ float t[64][65];
     const long long z = blockIdx.z;
     const Start s = start_of(parts + z * nparts, nparts, eps);
@@ -127,42 +154,48 @@ __global__ void __launch_bounds__(256) ortho_start(const void* G, Planes X, Plan
     const bool tall = m > n;
     // rows i0.. and columns j0.. of G, padded like it
     const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
-    const int cp = tall ? kp : rp, dp = tall ? rp : kp;  // padded columns and rows of G
-    Planes& P = tall ? XT : X;
-    Planes& Q = tall ? X : XT;
+    const Panels& P = tall ? XT : X;
+    const Panels& Q = tall ? X : XT;
     for (int e = threadIdx.x; e < 64 * 64; e += 256) {
         const int i = e / 64, j = e % 64;
         float g = 0.f;
         if (i0 + i < m && j0 + j < n)
-            g = (float)pack_load<DT, 1>(G, z * (long long)m * n + (long long)(i0 + i) * n + j0 + j).e[0];
-        g = g / s.top * inv;
-        if (i0 + i >= m || j0 + j >= n) g = 0.f;
+            g = (float)pack_load<DT, 1>(G, z * (long long)m * n + (long long)(i0 + i) * n + j0 + j).e[0] *
+                s.unit * inv;
         t[i][j] = g;
-        h16 hi, lo;
-        split(g, &hi, &lo);
-        const long long at = (long long)(i0 + i) * cp + j0 + j;
-        P.hi(z)[at] = hi;
-        P.lo(z)[at] = lo;
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
-        const int j = e / 64, i = e % 64;
-        h16 hi, lo;
-        split(t[i][j], &hi, &lo);
-        const long long at = (long long)(j0 + j) * dp + i0 + i;
-        Q.hi(z)[at] = hi;
-        Q.lo(z)[at] = lo;
+    // four elements of a row of P, and of Q
+    for (int e = threadIdx.x; e < 64 * 16; e += 256) {
+        const int i = e / 16, j = e % 16 * 4;
+        h16x4 hi, lo, th, tl;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            h16 a, b;
+            split(t[i][j + u], &a, &b);
+            hi[u] = a;
+            lo[u] = b;
+            split(t[j + u][i], &a, &b);
+            th[u] = a;
+            tl[u] = b;
+        }
+        h16* p = P.at(z, i0 + i, j0 + j);
+        *reinterpret_cast<h16x4*>(p) = hi;
+        *reinterpret_cast<h16x4*>(p + kLo) = lo;
+        h16* q = Q.at(z, j0 + i, i0 + j);
+        *reinterpret_cast<h16x4*>(q) = th;
+        *reinterpret_cast<h16x4*>(q + kLo) = tl;
     }
 }
 
 // With no steps: X itself.
 template <int DT>
-__global__ void __launch_bounds__(256) ortho_scaled(const void* G, void* X, const float2* parts,
+__global__ void __launch_bounds__(256) ortho_scaled(const void* G, void* X, const float4* parts,
                                                     int nparts, long long sz, float eps) {
     const long long z = blockIdx.y;
     const Start s = start_of(parts + z * nparts, nparts, eps);
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < sz; i += gridDim.x * 256LL) {
-        const float v[1] = {(float)pack_load<DT, 1>(G, z * sz + i).e[0] / s.top * s.inv};
+        const float v[1] = {(float)pack_load<DT, 1>(G, z * sz + i).e[0] * s.unit * s.inv};
         pack_store<DT, 1>(X, z * sz + i, v);
     }
 }
@@ -171,9 +204,9 @@ __global__ void __launch_bounds__(256) ortho_scaled(const void* G, void* X, cons
 enum { GRAM, POLY, APPLY };
 
 struct Product {
-    Planes P, Q;   // C[i, j] = sum_t P[i, t] Q[j, t]
-    Planes D, C;   // the own term and the result
-    Planes CT;     // APPLY: the result's transpose
+    Panels P, Q;   // C[i, j] = sum_t P[i, t] Q[j, t]
+    Panels D, C;   // the own term and the result
+    Panels CT;     // APPLY: the result's transpose
     void* out;     // last APPLY: X [m, n] instead
     int rows, cols, K;  // padded
     int m, n;
@@ -188,8 +221,8 @@ struct Product {
 template <int BM, int MODE, int OUT>
 __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, long long all) {
     constexpr int BK = 32, MT = BM / 64;
-    constexpr int LD = BM * 4 / 256;          // 16-byte chunks of a plane per thread
-    __shared__ h16 sm[2][2][2][BM * BK];      // buffer, operand, plane
+    constexpr int LD = BM * 8 / 256;          // 16-byte chunks of an operand per thread
+    __shared__ __attribute__((aligned(16))) h16 sm[2][2][BM * 2 * BK];  // buffer, operand
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long per = (all + 7) / 8, id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= per || id >= all) return;
@@ -207,68 +240,71 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
         while ((bj + 1) * (bj + 2) / 2 <= t) ++bj;
         bi = t - bj * (bj + 1) / 2;
     }
-    const h16* src[2][2] = {{g.P.hi(z), g.P.lo(z)}, {g.Q.hi(z), g.Q.lo(z)}};
-    const int row0[2] = {bi * BM, bj * BM};
+    const h16* src[2] = {g.P.at(z, bi * BM, 0), g.Q.at(z, bj * BM, 0)};
+    const long long next[2] = {g.P.rows * 64LL, g.Q.rows * 64LL};  // to the next panel
+    // Two steps' loads are on their way while one is worked on: a step's
+    // products take 0.6 us, a load under load longer.
     h16x8 st[2][2][LD];
-    auto fetch = [&](int k0) {
+    auto fetch = [&](h16x8 (&to)[2][LD], int s) {
 #pragma unroll
         for (int o = 0; o < 2; ++o)
 #pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-                for (int u = 0; u < LD; ++u) {
-                    const int q = threadIdx.x + 256 * u, row = q >> 2, c = q & 3;
-                    st[o][p][u] = *reinterpret_cast<const h16x8*>(
-                        src[o][p] + (long long)(row0[o] + row) * g.K + k0 + c * 8);
-                }
+            for (int u = 0; u < LD; ++u)
+                to[o][u] = *reinterpret_cast<const h16x8*>(src[o] + s * next[o] +
+                                                           (threadIdx.x + 256 * u) * 8);
     };
-    // chunk c of row `row` sits at c ^ (row / 4 mod 4): 16 rows that are read
-    // together then lie in different banks
-    auto place = [&](int b) {
+    // chunk c of a row (4 of hi, 4 of lo) sits at c ^ (row / 2 mod 8): 16 rows
+    // that are read together lie in different banks
+    auto chunk = [](int row, int c) { return row * 64 + (c ^ ((row >> 1) & 7)) * 8; };
+    auto place = [&](const h16x8 (&from)[2][LD], int b) {
 #pragma unroll
         for (int o = 0; o < 2; ++o)
 #pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-                for (int u = 0; u < LD; ++u) {
-                    const int q = threadIdx.x + 256 * u, row = q >> 2, c = q & 3;
-                    *reinterpret_cast<h16x8*>(&sm[b][o][p][row * BK + ((c ^ (row >> 2)) & 3) * 8]) =
-                        st[o][p][u];
-                }
+            for (int u = 0; u < LD; ++u) {
+                const int q = threadIdx.x + 256 * u;
+                *reinterpret_cast<h16x8*>(&sm[b][o][chunk(q >> 3, q & 7)]) = from[o][u];
+            }
     };
     const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BM / 2);
     const int r32 = lane & 31, half = lane >> 5;
     f32x16 acc[MT][MT] = {};
-    fetch(0);
-    place(0);
-    __syncthreads();
     const int steps = g.K / BK;
-    for (int s = 0; s < steps; ++s) {
-        if (s + 1 < steps) fetch((s + 1) * BK);
+    auto multiply = [&](int buf) {
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
             h16x8 a[MT][2], b[MT][2];
-            const int c = kk * 2 + half;
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
                 for (int p = 0; p < 2; ++p) {
-                    const int ra = wm + t * 32 + r32, rb = wn + t * 32 + r32;
-                    a[t][p] = *reinterpret_cast<const h16x8*>(
-                        &sm[s & 1][0][p][ra * BK + ((c ^ (ra >> 2)) & 3) * 8]);
-                    b[t][p] = *reinterpret_cast<const h16x8*>(
-                        &sm[s & 1][1][p][rb * BK + ((c ^ (rb >> 2)) & 3) * 8]);
+                    const int c = p * 4 + kk * 2 + half;
+                    a[t][p] = *reinterpret_cast<const h16x8*>(&sm[buf][0][chunk(wm + t * 32 + r32, c)]);
+                    b[t][p] = *reinterpret_cast<const h16x8*>(&sm[buf][1][chunk(wn + t * 32 + r32, c)]);
                 }
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+            for (int p = 0; p < 3; ++p)
 #pragma unroll
-                for (int j = 0; j < MT; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][1], b[j][0], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], b[j][1], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], b[j][0], acc[i][j], 0, 0, 0);
-                }
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < MT; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                            a[i][p == 0], b[j][p == 1], acc[i][j], 0, 0, 0);
         }
-        if (s + 1 < steps) place((s + 1) & 1);
+    };
+    // step s from buffer s & 1; the step after it waits in st[(s + 1) & 1]
+    fetch(st[0], 0);
+    if (steps > 1) fetch(st[1], 1);
+    place(st[0], 0);
+    __syncthreads();
+    for (int s = 0; s < steps; s += 2) {
+        if (s + 2 < steps) fetch(st[0], s + 2);
+        multiply(0);
+        if (s + 1 < steps) place(st[1], 1);
+        __syncthreads();
+        if (s + 1 >= steps) break;
+        if (s + 3 < steps) fetch(st[1], s + 3);
+        multiply(1);
+        if (s + 2 < steps) place(st[0], 0);
         __syncthreads();
     }
     // a lane holds column r32 of each 32 x 32 tile, rows 8 q + 4 half + 0 .. 3
@@ -300,8 +336,10 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     v[e] = f * acc[i][j][4 * q + e];
-                    const long long at = (long long)(row + e) * g.cols + col;
-                    if (MODE != GRAM) v[e] = fmaf(own, join(g.D.hi(z)[at], g.D.lo(z)[at]), v[e]);
+                    if (MODE != GRAM) {
+                        const h16* d = g.D.at(z, row + e, col);
+                        v[e] = fmaf(own, join(d[0], d[kLo]), v[e]);
+                    }
                     h16 a, b;
                     split(v[e], &a, &b);
                     hi[e] = a;
@@ -321,15 +359,14 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
                     // as rows, and as columns: the transpose, or the tile below the diagonal
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const long long at = (long long)(row + e) * g.cols + col;
-                        g.C.hi(z)[at] = hi[e];
-                        g.C.lo(z)[at] = lo[e];
+                        h16* c = g.C.at(z, row + e, col);
+                        c[0] = hi[e];
+                        c[kLo] = lo[e];
                     }
-                    const Planes& T = MODE == APPLY ? g.CT : g.C;
                     if (MODE == APPLY || bi != bj) {
-                        const long long at = (long long)col * g.rows + row;
-                        *reinterpret_cast<h16x4*>(T.hi(z) + at) = hi;
-                        *reinterpret_cast<h16x4*>(T.lo(z) + at) = lo;
+                        h16* c = (MODE == APPLY ? g.CT : g.C).at(z, col, row);
+                        *reinterpret_cast<h16x4*>(c) = hi;
+                        *reinterpret_cast<h16x4*>(c + kLo) = lo;
                     }
                 }
             }
@@ -556,7 +593,7 @@ int padded(int n) { return n >= 512 ? (n + 127) / 128 * 128 : (n + 63) / 64 * 64
 struct Plan {
     int k, r, kp, rp, parts;
     long long some;  // matrices at a time
-    size_t xs, as;   // bytes of a matrix's X and A planes
+    size_t xs, as;   // bytes of a matrix's X and A parts
 };
 Plan plan_of(int N, int m, int n) {
     Plan p;
@@ -624,13 +661,13 @@ hipError_t run(const void* G, void* X, int N, int m, int n, int steps, float ca,
         const int some = (int)std::min<long long>(p.some, N - at);
         const void* g = (const char*)G + at * sz * sizeof(elem_t<DT>);
         void* out = (char*)X + at * sz * sizeof(elem_t<DT>);
-        float2* parts = (float2*)ws;
+        float4* parts = (float4*)ws;
         float* depth = (float*)(parts + p.some * kParts);
-        char* q = ws + (size_t)p.some * (kParts + 32) * sizeof(float2);
+        char* q = ws + (size_t)p.some * (kParts + 16) * sizeof(float4);
         const long long xn = (long long)p.kp * p.rp, an = (long long)p.kp * p.kp;
-        const Planes x{(h16*)q, xn}, A{(h16*)(q + 3 * p.some * p.xs), an},
-            B{(h16*)(q + p.some * (3 * p.xs + p.as)), an};
-        Planes xt{(h16*)(q + p.some * p.xs), xn}, yt{(h16*)(q + 2 * p.some * p.xs), xn};
+        const Panels x{(h16*)q, xn, p.kp}, A{(h16*)(q + 3 * p.some * p.xs), an, p.kp},
+            B{(h16*)(q + p.some * (3 * p.xs + p.as)), an, p.kp};
+        Panels xt{(h16*)(q + p.some * p.xs), xn, p.rp}, yt{(h16*)(q + 2 * p.some * p.xs), xn, p.rp};
         ortho_norm<DT><<<dim3(p.parts, some), 256, 0, st>>>(g, parts, sz);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -643,7 +680,7 @@ hipError_t run(const void* G, void* X, int N, int m, int n, int steps, float ca,
         }
         const int gr = m > n ? p.rp : p.kp, gc = m > n ? p.kp : p.rp;
         ortho_start<DT><<<dim3(gc / 64, gr / 64, some), 256, 0, st>>>(g, x, xt, parts, p.parts,
-                                                                      depth, m, n, p.kp, p.rp, eps);
+                                                                      depth, m, n, eps);
         e = hipGetLastError();
         for (int s = 0; s < steps && e == hipSuccess; ++s) {
             e = product<GRAM, -1>({x, x, {}, A, {}, nullptr, p.kp, p.kp, p.rp, m, n, depth,
@@ -669,7 +706,7 @@ hipError_t run(const void* G, void* X, int N, int m, int n, int steps, float ca,
 size_t ortho_workspace(int N, int m, int n) {
     if (small_side(m, n)) return 256;
     const Plan p = plan_of(N, m, n);
-    return (size_t)p.some * ((kParts + 32) * sizeof(float2) + 3 * p.xs + 2 * p.as);
+    return (size_t)p.some * ((kParts + 16) * sizeof(float4) + 3 * p.xs + 2 * p.as);
 }
 
 hipError_t launch_ortho(const void* G, void* X, int N, int m, int n, int steps, float ca, float cb,
