@@ -41,6 +41,41 @@ __device__ __forceinline__ float join(h16 hi, h16 lo) {
     return ((float)hi + (float)lo) * kUnscale;
 }
 
+// Four rows of a lane's column <-> row lane % 4 of them, of the four columns of
+// the lane's quad (its own inverse): two exchanges inside the quad, elements two to a register.
+__device__ __forceinline__ h16x4 quad_turn(h16x4 v) {
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 w = __builtin_bit_cast(u32x2, v);
+    const bool odd = threadIdx.x & 1, upper = threadIdx.x & 2;
+    // even lanes: the first of each pair of rows, odd lanes the second
+    const unsigned sel = odd ? 0x03020706u : 0x05040100u;
+    unsigned a = __builtin_amdgcn_perm(
+        __builtin_amdgcn_update_dpp(0u, w.x, 0xB1, 0xF, 0xF, false), w.x, sel);
+    unsigned b = __builtin_amdgcn_perm(
+        __builtin_amdgcn_update_dpp(0u, w.y, 0xB1, 0xF, 0xF, false), w.y, sel);
+    // the lower two lanes keep the first two rows, the upper two the others
+    const unsigned got = __builtin_amdgcn_update_dpp(0u, upper ? a : b, 0x4E, 0xF, 0xF, false);
+    return __builtin_bit_cast(h16x4, upper ? u32x2{got, b} : u32x2{a, got});
+}
+
+// Rows 8 q + 4 half + 0 .. 3 for q = 0, 1 of a lane's column <-> rows 8 half +
+// 0 .. 7, by an exchange between the halves of the wave (its own inverse).
+__device__ __forceinline__ void half_turn(h16x4* p, h16x4* q) {
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 a = __builtin_bit_cast(u32x2, *p), b = __builtin_bit_cast(u32x2, *q);
+    const auto x = __builtin_amdgcn_permlane32_swap(a.x, b.x, false, false);
+    const auto y = __builtin_amdgcn_permlane32_swap(a.y, b.y, false, false);
+    *p = __builtin_bit_cast(h16x4, u32x2{x[0], y[0]});
+    *q = __builtin_bit_cast(h16x4, u32x2{x[1], y[1]});
+}
+
+// Reads LDS across its rows (see where it is used).
+__device__ __forceinline__ h16x4 read_across(const h16* p) {
+    typedef __fp16 f16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) f16x4* Lds;
+    return __builtin_bit_cast(h16x4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((Lds)p));
+}
+
 // ------------------------------------------------------------------ the start
 constexpr int kParts = 64;  // most workgroups that share a matrix's norm
 // Squares are summed in units of 2^160, 1 and 2^-160; to the next larger unit:
@@ -141,11 +176,11 @@ struct Panels {
 };
 constexpr int kLo = 32;  // from hi to lo
 
-// X [kp, rp] and its transpose XT from G [m, n], 64 x 64 at a time.
+// X [kp, rp] from G [m, n] (its transpose where m > n), 64 x 64 at a time.
 template <int DT>
-__global__ void __launch_bounds__(256) ortho_start(const void* G, Panels X, Panels XT,
-                                                   const float4* parts, int nparts, float* depth,
-                                                   int m, int n, float eps) {
+__global__ void __launch_bounds__(256) ortho_start(const void* G, Panels X, const float4* parts,
+                                                   int nparts, float* depth, int m, int n,
+                                                   float eps) {
     __shared__ float t[64][65];
     const long long z = blockIdx.z;
     const Start s = start_of(parts + z * nparts, nparts, eps);
@@ -154,8 +189,6 @@ __global__ void __launch_bounds__(256) ortho_start(const void* G, Panels X, Pane
     const bool tall = m > n;
     // rows i0.. and columns j0.. of G, padded like it
     const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
-    const Panels& P = tall ? XT : X;
-    const Panels& Q = tall ? X : XT;
     for (int e = threadIdx.x; e < 64 * 64; e += 256) {
         const int i = e / 64, j = e % 64;
         float g = 0.f;
@@ -165,26 +198,20 @@ __global__ void __launch_bounds__(256) ortho_start(const void* G, Panels X, Pane
         t[i][j] = g;
     }
     __syncthreads();
-    // four elements of a row of P, and of Q
+    // four elements of a row
     for (int e = threadIdx.x; e < 64 * 16; e += 256) {
         const int i = e / 16, j = e % 16 * 4;
-        h16x4 hi, lo, th, tl;
+        h16x4 hi, lo;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             h16 a, b;
-            split(t[i][j + u], &a, &b);
+            split(tall ? t[j + u][i] : t[i][j + u], &a, &b);
             hi[u] = a;
             lo[u] = b;
-            split(t[j + u][i], &a, &b);
-            th[u] = a;
-            tl[u] = b;
         }
-        h16* p = P.at(z, i0 + i, j0 + j);
+        h16* p = tall ? X.at(z, j0 + i, i0 + j) : X.at(z, i0 + i, j0 + j);
         *reinterpret_cast<h16x4*>(p) = hi;
         *reinterpret_cast<h16x4*>(p + kLo) = lo;
-        h16* q = Q.at(z, j0 + i, i0 + j);
-        *reinterpret_cast<h16x4*>(q) = th;
-        *reinterpret_cast<h16x4*>(q + kLo) = tl;
     }
 }
 
@@ -204,9 +231,8 @@ __global__ void __launch_bounds__(256) ortho_scaled(const void* G, void* X, cons
 enum { GRAM, POLY, APPLY };
 
 struct Product {
-    Panels P, Q;   // C[i, j] = sum_t P[i, t] Q[j, t]
-    Panels D, C;   // the own term and the result
-    Panels CT;     // APPLY: the result's transpose
+    Panels P, Q;   // C[i, j] = sum_t P[i, t] Q[j, t], APPLY: sum_t P[i, t] Q[t, j]
+    Panels C;      // the result; its own term D is A = P = Q, APPLY: X = Q
     void* out;     // last APPLY: X [m, n] instead
     int rows, cols, K;  // padded
     int m, n;
@@ -240,8 +266,12 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
         while ((bj + 1) * (bj + 2) / 2 <= t) ++bj;
         bi = t - bj * (bj + 1) / 2;
     }
-    const h16* src[2] = {g.P.at(z, bi * BM, 0), g.Q.at(z, bj * BM, 0)};
-    const long long next[2] = {g.P.rows * 64LL, g.Q.rows * 64LL};  // to the next panel
+    // An operand's tile in a step: BM rows of one panel, or (APPLY's right one)
+    // 32 rows of BM / 32 panels, whose columns are read across.
+    constexpr bool ACROSS = MODE == APPLY;
+    const h16* src[2] = {g.P.at(z, bi * BM, 0),
+                         ACROSS ? g.Q.at(z, 0, bj * BM) : g.Q.at(z, bj * BM, 0)};
+    const long long ahead[2] = {g.P.rows * 64LL, ACROSS ? 32 * 64LL : g.Q.rows * 64LL};
     // Two steps' loads are on their way while one is worked on: a step's
     // products take 0.6 us, a load under load longer.
     h16x8 st[2][2][LD];
@@ -249,9 +279,12 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
 #pragma unroll
         for (int o = 0; o < 2; ++o)
 #pragma unroll
-            for (int u = 0; u < LD; ++u)
-                to[o][u] = *reinterpret_cast<const h16x8*>(src[o] + s * next[o] +
-                                                           (threadIdx.x + 256 * u) * 8);
+            for (int u = 0; u < LD; ++u) {
+                const int q = threadIdx.x + 256 * u;
+                const long long at = ACROSS && o == 1 ? (q >> 8) * (g.Q.rows * 64LL) + (q & 255) * 8
+                                                      : q * 8;
+                to[o][u] = *reinterpret_cast<const h16x8*>(src[o] + s * ahead[o] + at);
+            }
     };
     // chunk c of a row (4 of hi, 4 of lo) sits at c ^ (row / 2 mod 8): 16 rows
     // that are read together lie in different banks
@@ -279,7 +312,21 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
                 for (int p = 0; p < 2; ++p) {
                     const int c = p * 4 + kk * 2 + half;
                     a[t][p] = *reinterpret_cast<const h16x8*>(&sm[buf][0][chunk(wm + t * 32 + r32, c)]);
-                    b[t][p] = *reinterpret_cast<const h16x8*>(&sm[buf][1][chunk(wn + t * 32 + r32, c)]);
+                    if constexpr (ACROSS) {
+                        // lane 4 i + j of 16 gives row i, columns 4 j .. 4 j + 3 of a 4 x 16
+                        // block and gets its column 4 i + j
+                        h16x4 v[2];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const int k = wn + t * 32 + kk * 16 + half * 8 + u * 4 + ((lane & 15) >> 2);
+                            const int x = (lane & 16) + (lane & 3) * 4;
+                            v[u] = read_across(&sm[buf][1][chunk(k, p * 4 + (x >> 3)) + (x & 7)]);
+                        }
+                        b[t][p] = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                    } else {
+                        b[t][p] = *reinterpret_cast<const h16x8*>(
+                            &sm[buf][1][chunk(wn + t * 32 + r32, c)]);
+                    }
                 }
 #pragma unroll
             for (int p = 0; p < 3; ++p)
@@ -326,50 +373,64 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < MT; ++j)
+        for (int j = 0; j < MT; ++j) {
+            const int row0 = bi * BM + wm + i * 32, col = bj * BM + wn + j * 32 + r32;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int row = bi * BM + wm + i * 32 + 8 * q + 4 * half;
-                const int col = bj * BM + wn + j * 32 + r32;
-                h16x4 hi, lo;
-                float v[4];
+            for (int q = 0; q < 4; q += 2) {
+                h16x4 own_hi[2], own_lo[2];
+                if constexpr (MODE == POLY) {
+                    // by symmetry 8 columns of a row: one load
+                    const h16* d = g.P.at(z, col, row0 + 8 * (q + half));
+                    const h16x8 dh = *reinterpret_cast<const h16x8*>(d);
+                    const h16x8 dl = *reinterpret_cast<const h16x8*>(d + kLo);
+                    own_hi[0] = dh.lo, own_hi[1] = dh.hi, own_lo[0] = dl.lo, own_lo[1] = dl.hi;
+                    half_turn(&own_hi[0], &own_hi[1]);
+                    half_turn(&own_lo[0], &own_lo[1]);
+                } else if constexpr (MODE == APPLY) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[e] = f * acc[i][j][4 * q + e];
-                    if (MODE != GRAM) {
-                        const h16* d = g.D.at(z, row + e, col);
-                        v[e] = fmaf(own, join(d[0], d[kLo]), v[e]);
+                    for (int u = 0; u < 2; ++u) {
+                        const h16* d = g.Q.at(z, row0 + 8 * (q + u) + 4 * half + (lane & 3), col & ~3);
+                        own_hi[u] = quad_turn(*reinterpret_cast<const h16x4*>(d));
+                        own_lo[u] = quad_turn(*reinterpret_cast<const h16x4*>(d + kLo));
                     }
-                    h16 a, b;
-                    split(v[e], &a, &b);
-                    hi[e] = a;
-                    lo[e] = b;
                 }
-                if constexpr (OUT >= 0) {
+                h16x4 hi[2], lo[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int row = row0 + 8 * (q + u) + 4 * half;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float one[1] = {ldexpf(v[e], fin)};
-                        const bool tall = g.m > g.n;
-                        const int r = tall ? col : row + e, c = tall ? row + e : col;
-                        if (r < g.m && c < g.n)
-                            pack_store<OUT < 0 ? 0 : OUT, 1>(
-                                g.out, (z * g.m + r) * (long long)g.n + c, one);
+                        float v = f * acc[i][j][4 * (q + u) + e];
+                        if (MODE != GRAM) v = fmaf(own, join(own_hi[u][e], own_lo[u][e]), v);
+                        if constexpr (OUT >= 0) {
+                            const float one[1] = {ldexpf(v, fin)};
+                            const bool tall = g.m > g.n;
+                            const int r = tall ? col : row + e, c = tall ? row + e : col;
+                            if (r < g.m && c < g.n)
+                                pack_store<OUT < 0 ? 0 : OUT, 1>(
+                                    g.out, (z * g.m + r) * (long long)g.n + c, one);
+                        }
+                        h16 a, b;
+                        split(v, &a, &b);
+                        hi[u][e] = a;
+                        lo[u][e] = b;
                     }
-                } else {
-                    // as rows, and as columns: the transpose, or the tile below the diagonal
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        h16* c = g.C.at(z, row + e, col);
-                        c[0] = hi[e];
-                        c[kLo] = lo[e];
+                    if (OUT < 0 && (MODE == APPLY || bi != bj)) {
+                        h16* c = g.C.at(z, row + (lane & 3), col & ~3);
+                        *reinterpret_cast<h16x4*>(c) = quad_turn(hi[u]);
+                        *reinterpret_cast<h16x4*>(c + kLo) = quad_turn(lo[u]);
                     }
-                    if (MODE == APPLY || bi != bj) {
-                        h16* c = (MODE == APPLY ? g.CT : g.C).at(z, col, row);
-                        *reinterpret_cast<h16x4*>(c) = hi;
-                        *reinterpret_cast<h16x4*>(c + kLo) = lo;
-                    }
+                }
+                if constexpr (MODE != APPLY) {
+                    // by symmetry the tile across the diagonal
+                    half_turn(&hi[0], &hi[1]);
+                    half_turn(&lo[0], &lo[1]);
+                    h16* c = g.C.at(z, col, row0 + 8 * (q + half));
+                    *reinterpret_cast<h16x8*>(c) = __builtin_shufflevector(hi[0], hi[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                    *reinterpret_cast<h16x8*>(c + kLo) = __builtin_shufflevector(lo[0], lo[1], 0, 1, 2, 3, 4, 5, 6, 7);
                 }
             }
+        }
 }
 
 // ----------------------------------------------------------- small matrices
@@ -500,10 +561,11 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
             for (int t = 0; t < NT; ++t)
                 if (t < rt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int at = row_of(t, i / 4, i % 4) * PITCH + col;
-                        sm[0][at] = xh[t][i / 8][i % 8];
-                        sm[1][at] = xl[t][i / 8][i % 8];
+                    for (int q = 0; q < 4; ++q) {
+                        const int at = row_of(t, q, lane & 3) * PITCH + (col & ~3);
+                        const h16x8 h = xh[t][q / 2], l = xl[t][q / 2];
+                        *reinterpret_cast<h16x4*>(&sm[0][at]) = quad_turn(q & 1 ? h.hi : h.lo);
+                        *reinterpret_cast<h16x4*>(&sm[1][at]) = quad_turn(q & 1 ? l.hi : l.lo);
                     }
         __syncthreads();
         if (square) product(rs, own_rows);
@@ -593,7 +655,7 @@ int padded(int n) { return n >= 512 ? (n + 127) / 128 * 128 : (n + 63) / 64 * 64
 struct Plan {
     int k, r, kp, rp, parts;
     long long some;  // matrices at a time
-    size_t xs, as;   // bytes of a matrix's X and A parts
+    size_t xs;       // bytes of a matrix's parts
 };
 Plan plan_of(int N, int m, int n) {
     Plan p;
@@ -602,9 +664,8 @@ Plan plan_of(int N, int m, int n) {
     p.kp = padded(p.k);
     p.rp = padded(p.r);
     p.xs = (size_t)p.kp * p.rp * 4;
-    p.as = (size_t)p.kp * p.kp * 4;
     p.parts = (int)std::min<long long>(kParts, ((long long)m * n + 16383) / 16384);
-    const size_t each = 3 * p.xs + 2 * p.as;
+    const size_t each = 3 * p.xs;
     p.some = std::max<long long>(1, std::min<long long>({N, 32768, (long long)((1ull << 30) / each)}));
     return p;
 }
@@ -664,10 +725,10 @@ hipError_t run(const void* G, void* X, int N, int m, int n, int steps, float ca,
         float4* parts = (float4*)ws;
         float* depth = (float*)(parts + p.some * kParts);
         char* q = ws + (size_t)p.some * (kParts + 16) * sizeof(float4);
+        // X, A and B take turns in three buffers of X's size
         const long long xn = (long long)p.kp * p.rp, an = (long long)p.kp * p.kp;
-        const Panels x{(h16*)q, xn, p.kp}, A{(h16*)(q + 3 * p.some * p.xs), an, p.kp},
-            B{(h16*)(q + p.some * (3 * p.xs + p.as)), an, p.kp};
-        Panels xt{(h16*)(q + p.some * p.xs), xn, p.rp}, yt{(h16*)(q + 2 * p.some * p.xs), xn, p.rp};
+        h16* buf[3];
+        for (int i = 0; i < 3; ++i) buf[i] = (h16*)(q + i * p.some * p.xs);
         ortho_norm<DT><<<dim3(p.parts, some), 256, 0, st>>>(g, parts, sz);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -679,22 +740,22 @@ hipError_t run(const void* G, void* X, int N, int m, int n, int steps, float ca,
             continue;
         }
         const int gr = m > n ? p.rp : p.kp, gc = m > n ? p.kp : p.rp;
-        ortho_start<DT><<<dim3(gc / 64, gr / 64, some), 256, 0, st>>>(g, x, xt, parts, p.parts,
-                                                                      depth, m, n, eps);
+        ortho_start<DT><<<dim3(gc / 64, gr / 64, some), 256, 0, st>>>(
+            g, Panels{buf[0], xn, p.kp}, parts, p.parts, depth, m, n, eps);
         e = hipGetLastError();
         for (int s = 0; s < steps && e == hipSuccess; ++s) {
-            e = product<GRAM, -1>({x, x, {}, A, {}, nullptr, p.kp, p.kp, p.rp, m, n, depth,
-                                   rate, s, 0.f, 1.f},
+            const Panels x{buf[0], xn, p.kp}, A{buf[1], an, p.kp}, B{buf[2], an, p.kp},
+                y{buf[1], xn, p.kp};  // over A
+            e = product<GRAM, -1>({x, x, A, nullptr, p.kp, p.kp, p.rp, m, n, depth, rate, s, 0.f, 1.f},
                                   some, st);
             if (e == hipSuccess)
-                e = product<POLY, -1>({A, A, A, B, {}, nullptr, p.kp, p.kp, p.kp, m, n, depth,
-                                       rate, s, cb, cc},
+                e = product<POLY, -1>({A, A, B, nullptr, p.kp, p.kp, p.kp, m, n, depth, rate, s, cb, cc},
                                       some, st);
-            const Product last{B, xt, x, x, yt, out, p.kp, p.rp, p.kp, m, n, depth, rate, s, ca, 1.f};
+            const Product last{B, x, y, out, p.kp, p.rp, p.kp, m, n, depth, rate, s, ca, 1.f};
             if (e == hipSuccess)
                 e = s + 1 < steps ? product<APPLY, -1>(last, some, st)
                                   : product<APPLY, DT>(last, some, st);
-            std::swap(xt, yt);
+            std::swap(buf[0], buf[1]);
         }
         if (e != hipSuccess) return e;
     }
@@ -706,7 +767,7 @@ hipError_t run(const void* G, void* X, int N, int m, int n, int steps, float ca,
 size_t ortho_workspace(int N, int m, int n) {
     if (small_side(m, n)) return 256;
     const Plan p = plan_of(N, m, n);
-    return (size_t)p.some * ((kParts + 16) * sizeof(float4) + 3 * p.xs + 2 * p.as);
+    return (size_t)p.some * ((kParts + 16) * sizeof(float4) + 3 * p.xs);
 }
 
 hipError_t launch_ortho(const void* G, void* X, int N, int m, int n, int steps, float ca, float cb,
