@@ -8,6 +8,7 @@ raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 
@@ -492,12 +493,38 @@ def deeppcr_seq_backward(W, bias, z0, Z, G, layer: int = TANH_MLP, alpha: float 
 
 
 # ------------------------------------------------ recurrent language models
-def _dtype_code(t, name):
+# A step of one token is a few microseconds on the GPU: what these calls do on
+# the host is kept short (library functions and sizes looked up once, addresses
+# passed as integers).
+@functools.lru_cache(maxsize=None)
+def _codes():
     torch = _torch()
-    code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(t.dtype)
+    return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+@functools.lru_cache(maxsize=None)
+def _entry(name):
+    return getattr(lib(), name)
+
+
+@functools.lru_cache(maxsize=None)
+def _raw_stream():
+    """The handle of a device's current stream, without a Python object for the
+    stream where torch has that (2.5 us less per call)."""
+    torch = _torch()
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _dtype_code(t, name):
+    code = _codes().get(t.dtype)
     if code is None:
         raise ValueError(f"{name} must be float32, bfloat16 or float16, not {t.dtype}")
     return code
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _rows(t, shape, name, like):
@@ -506,9 +533,11 @@ def _rows(t, shape, name, like):
     returns that stride."""
     if t.dtype != like.dtype or t.device != like.device or not t.is_cuda:
         raise ValueError(f"{name} must be a {like.dtype} GPU tensor on {like.device}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     w = shape[-1]
+    if t.is_contiguous():
+        return w
     ld, n = None, 1
     for size, stride in zip(reversed(shape[:-1]), reversed(t.stride()[:-1])):
         if size > 1:
@@ -529,35 +558,40 @@ def _typed(t, shape, name, dtype, device):
         return
     if t.dtype != dtype or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor on {device}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
 def _launch(name, stream, device, args, made):
     """Calls entry point `name` with `args` and the stream, on `device`; what
     the binding allocated (`made`) stays allocated until the stream is past it."""
-    torch = _torch()
-    with torch.cuda.device(device):
-        s = torch.cuda.current_stream(device) if stream is None else stream
-        st = getattr(lib(), name)(*args, ctypes.c_void_p(s.cuda_stream))
-        if stream is not None:
-            for t in made:
-                if t is not None:
-                    t.record_stream(stream)
+    cuda = _torch().cuda
+    if cuda.current_device() != device.index:
+        with cuda.device(device):
+            return _launch(name, stream, device, args, made)
+    if stream is None:
+        st = _entry(name)(*args, _raw_stream()(device.index))
+    else:
+        if stream.device != device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+        st = _entry(name)(*args, stream.cuda_stream)
+        for t in made:
+            t.record_stream(stream)
     if st != OK:
         raise DeepPCRError(st, name)
 
 
 def _space(workspace, nbytes, device, made):
-    torch = _torch()
     if workspace is None:
-        workspace = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
+        workspace = _torch().empty(max(nbytes, 1), dtype=_torch().uint8, device=device)
         made.append(workspace)
+        return workspace, nbytes
     if workspace.device != device or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {device}")
     return workspace, workspace.numel() * workspace.element_size()
 
 
+@functools.lru_cache(maxsize=1024)
 def gated_scan_workspace_bytes(B: int, L: int, w: int) -> int:
     return int(lib().deeppcr_gated_scan_workspace_bytes(B, L, w))
 
@@ -584,8 +618,8 @@ def deeppcr_gated_scan_forward(a, u, x0=None, lengths=None, gate: int = GATE_DIR
     _typed(x_last, (B, w), "x_last", torch.float32, dev)
     ws, nbytes = _space(workspace, gated_scan_workspace_bytes(B, L, w), dev, made)
     _launch("deeppcr_gated_scan_forward", stream, dev,
-            (_ptr(a), lda, _ptr(u), ldu, _ptr(x0), _ptr(lengths), _ptr(x), _ptr(x_last), B, L, w,
-             int(gate), dt, _ptr(ws), nbytes), made)
+            (_addr(a), lda, _addr(u), ldu, _addr(x0), _addr(lengths), _addr(x), _addr(x_last), B, L, w,
+             int(gate), dt, _addr(ws), nbytes), made)
     return x, x_last
 
 
@@ -620,8 +654,8 @@ def deeppcr_gated_scan_backward(a, u, x, g, g_last=None, x0=None, lengths=None,
     _typed(dx0, (B, w), "dx0", torch.float32, dev)
     ws, nbytes = _space(workspace, gated_scan_workspace_bytes(B, L, w), dev, made)
     _launch("deeppcr_gated_scan_backward", stream, dev,
-            (_ptr(a), lda, _ptr(u), ldu, _ptr(x), _ptr(x0), _ptr(lengths), _ptr(g), ldg,
-             _ptr(g_last), _ptr(da), _ptr(du), _ptr(dx0), B, L, w, int(gate), dt, _ptr(ws),
+            (_addr(a), lda, _addr(u), ldu, _addr(x), _addr(x0), _addr(lengths), _addr(g), ldg,
+             _addr(g_last), _addr(da), _addr(du), _addr(dx0), B, L, w, int(gate), dt, _addr(ws),
              nbytes), made)
     return da, du, dx0
 
@@ -645,7 +679,7 @@ def deeppcr_gated_scan_step(a, u, state, gate: int = GATE_DIRECT, x=None, state_
     _typed(state_out, (B, w), "state_out", torch.float32, dev)
     _typed(x, (B, w), "x", a.dtype, dev)
     _launch("deeppcr_gated_scan_step", stream, dev,
-            (_ptr(a), lda, _ptr(u), ldu, _ptr(state), _ptr(state_out), _ptr(x), B, w, int(gate),
+            (_addr(a), lda, _addr(u), ldu, _addr(state), _addr(state_out), _addr(x), B, w, int(gate),
              dt), made)
     return x
 
@@ -668,6 +702,7 @@ class NormGrads:
     dw_pre: object
 
 
+@functools.lru_cache(maxsize=1024)
 def residual_norm_workspace_bytes(B: int, L: int, w: int, z_per_seq: bool = False) -> int:
     return int(lib().deeppcr_residual_norm_workspace_bytes(B, L, w, int(bool(z_per_seq))))
 
@@ -711,8 +746,8 @@ def deeppcr_residual_norm_forward(x, y=None, z=None, w_post=None, scale=None, w_
     rpost = new((B, L), torch.float32) if w_post is not None else None
     rpre = new((B, L), torch.float32) if w_pre is not None else None
     _launch("deeppcr_residual_norm_forward", stream, x.device,
-            (_ptr(x), _ptr(y), ldy, _ptr(z), ldz, _ptr(w_post), _ptr(scale), _ptr(w_pre),
-             _ptr(x_out), _ptr(h), _ptr(rpost), _ptr(rpre), B, L, w, int(gate), per_seq,
+            (_addr(x), _addr(y), ldy, _addr(z), ldz, _addr(w_post), _addr(scale), _addr(w_pre),
+             _addr(x_out), _addr(h), _addr(rpost), _addr(rpre), B, L, w, int(gate), per_seq,
              float(eps), dt), made)
     return NormResult(x_out if y is not None else x, h, rpost, rpre)
 
@@ -745,13 +780,14 @@ def deeppcr_residual_norm_backward(x, y=None, rstd_post=None, rstd_pre=None, dx_
     dpost, dscale, dpre = (out(None, p, "", torch.float32) for p in (w_post, scale, w_pre))
     ws, nbytes = _space(workspace, residual_norm_workspace_bytes(B, L, w, per_seq), dev, made)
     _launch("deeppcr_residual_norm_backward", stream, dev,
-            (_ptr(x), _ptr(y), ldy, _ptr(z), ldz, _ptr(w_post), _ptr(scale), _ptr(w_pre),
-             _ptr(rstd_post), _ptr(rstd_pre), _ptr(dx_out), _ptr(dh), _ptr(dx), _ptr(dy),
-             _ptr(dz), _ptr(dpost), _ptr(dscale), _ptr(dpre), B, L, w, int(gate), per_seq, dt,
-             _ptr(ws), nbytes), made)
+            (_addr(x), _addr(y), ldy, _addr(z), ldz, _addr(w_post), _addr(scale), _addr(w_pre),
+             _addr(rstd_post), _addr(rstd_pre), _addr(dx_out), _addr(dh), _addr(dx), _addr(dy),
+             _addr(dz), _addr(dpost), _addr(dscale), _addr(dpre), B, L, w, int(gate), per_seq, dt,
+             _addr(ws), nbytes), made)
     return NormGrads(dx, dy, dz, dpost, dscale, dpre)
 
 
+@functools.lru_cache(maxsize=1024)
 def orthogonalize_workspace_bytes(N: int, m: int, n: int) -> int:
     return int(lib().deeppcr_orthogonalize_workspace_bytes(N, m, n))
 
@@ -775,7 +811,7 @@ def deeppcr_orthogonalize(G, X=None, steps: int = 5, coeffs=(3.4445, -4.7750, 2.
     ws, nbytes = _space(workspace, orthogonalize_workspace_bytes(N, m, n), G.device, made)
     ca, cb, cc = (float(c) for c in coeffs)
     _launch("deeppcr_orthogonalize", stream, G.device,
-            (_ptr(G), _ptr(X), N, m, n, int(steps), ca, cb, cc, float(eps), dt, _ptr(ws), nbytes),
+            (_addr(G), _addr(X), N, m, n, int(steps), ca, cb, cc, float(eps), dt, _addr(ws), nbytes),
             made)
     return X
 
