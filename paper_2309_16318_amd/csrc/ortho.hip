@@ -32,13 +32,24 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kScale = 1024.f, kUnscale = 1.f / 1024.f;  // 2^10
 
-__device__ __forceinline__ void split(float x, h16* hi, h16* lo) {
-    const float s = x * kScale;
-    *hi = (h16)s;
-    *lo = (h16)(s - (float)*hi);
+// The parts of four values that are already multiplied by kScale: two packed
+// conversions and two mixed-precision multiply-adds a pair (the matrix cores
+// and these instructions share a wave's issue slots).
+__device__ __forceinline__ void split(const float (&s)[4], h16x4* hi, h16x4* lo) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef h16 h16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+        const h16x2 h = __builtin_convertvector((f32x2{s[i], s[i + 1]}), h16x2);
+        const f32x2 r{fmaf((float)h.x, -1.f, s[i]), fmaf((float)h.y, -1.f, s[i + 1])};
+        const h16x2 l = __builtin_convertvector(r, h16x2);
+        (*hi)[i] = h.x, (*hi)[i + 1] = h.y;
+        (*lo)[i] = l.x, (*lo)[i + 1] = l.y;
+    }
 }
-__device__ __forceinline__ float join(h16 hi, h16 lo) {
-    return ((float)hi + (float)lo) * kUnscale;
+// own (hi + lo) + v
+__device__ __forceinline__ float add_own(float own, h16 hi, h16 lo, float v) {
+    return fmaf((float)hi, own, fmaf((float)lo, own, v));
 }
 
 // Four rows of a lane's column <-> row lane % 4 of them, of the four columns of
@@ -202,13 +213,10 @@ __global__ void __launch_bounds__(256) ortho_start(const void* G, Panels X, cons
     for (int e = threadIdx.x; e < 64 * 16; e += 256) {
         const int i = e / 16, j = e % 16 * 4;
         h16x4 hi, lo;
+        float v[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            h16 a, b;
-            split(tall ? t[j + u][i] : t[i][j + u], &a, &b);
-            hi[u] = a;
-            lo[u] = b;
-        }
+        for (int u = 0; u < 4; ++u) v[u] = kScale * (tall ? t[j + u][i] : t[i][j + u]);
+        split(v, &hi, &lo);
         h16* p = tall ? X.at(z, j0 + i, i0 + j) : X.at(z, i0 + i, j0 + j);
         *reinterpret_cast<h16x4*>(p) = hi;
         *reinterpret_cast<h16x4*>(p + kLo) = lo;
@@ -355,7 +363,8 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
         __syncthreads();
     }
     // a lane holds column r32 of each 32 x 32 tile, rows 8 q + 4 half + 0 .. 3
-    float own = g.own, f = g.times * kUnscale * kUnscale;
+    // values times kScale, as their parts are
+    float own = g.own, f = g.times * kUnscale;
     int fin = 0;
     if constexpr (MODE != GRAM) {
         const int e = shift_of(g.depth[z], g.rate, g.step);
@@ -398,23 +407,21 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const int row = row0 + 8 * (q + u) + 4 * half;
+                    float v[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float v = f * acc[i][j][4 * (q + u) + e];
-                        if (MODE != GRAM) v = fmaf(own, join(own_hi[u][e], own_lo[u][e]), v);
+                        v[e] = f * acc[i][j][4 * (q + u) + e];
+                        if (MODE != GRAM) v[e] = add_own(own, own_hi[u][e], own_lo[u][e], v[e]);
                         if constexpr (OUT >= 0) {
-                            const float one[1] = {ldexpf(v, fin)};
+                            const float one[1] = {ldexpf(v[e] * kUnscale, fin)};
                             const bool tall = g.m > g.n;
                             const int r = tall ? col : row + e, c = tall ? row + e : col;
                             if (r < g.m && c < g.n)
                                 pack_store<OUT < 0 ? 0 : OUT, 1>(
                                     g.out, (z * g.m + r) * (long long)g.n + c, one);
                         }
-                        h16 a, b;
-                        split(v, &a, &b);
-                        hi[u][e] = a;
-                        lo[u][e] = b;
                     }
+                    if (OUT < 0) split(v, &hi[u], &lo[u]);
                     if (OUT < 0 && (MODE == APPLY || bi != bj)) {
                         h16* c = g.C.at(z, row + (lane & 3), col & ~3);
                         *reinterpret_cast<h16x4*>(c) = quad_turn(hi[u]);
@@ -504,15 +511,24 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
     }
     inv = ldexpf(inv, shift_of(depth, 0.f, 0));
     h16x8 xh[NT][2], xl[NT][2];
+    // X's parts from four values times kScale
+    auto keep = [&](int t, int q, const float (&v)[4]) {
+        h16x4 hi, lo;
+        split(v, &hi, &lo);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            xh[t][q / 2][4 * (q & 1) + e] = hi[e];
+            xl[t][q / 2][4 * (q & 1) + e] = lo[e];
+        }
+    };
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            acc[t][i] *= inv;
-            h16 hi, lo;
-            split(acc[t][i], &hi, &lo);
-            xh[t][i / 8][i % 8] = hi;
-            xl[t][i / 8][i % 8] = lo;
+        for (int q = 0; q < 4; ++q) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = acc[t][4 * q + e] *= inv, v[e] *= kScale;
+            keep(t, q, v);
         }
 
     // acc = sum over `count` steps of 16 of rows (32 t ..) of LDS against `right`
@@ -551,7 +567,7 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
     auto run_of = [&](int t, int q) {
         return col * PITCH + 32 * t + 16 * (q >> 1) + 4 * (2 * half + (q & 1));
     };
-    const float f = kUnscale * kUnscale;
+    const float f = kUnscale;  // of a product, for a value times kScale
     for (int s = 0; s < steps; ++s) {
         const int e = shift_of(depth, rate, s);
         const bool square = 32 * wave < k, wide = 32 * wave < r;
@@ -577,13 +593,10 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         h16x4 hi, lo;
+                        float v[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            h16 a, b;
-                            split(times * acc[t][4 * q + i], &a, &b);
-                            hi[i] = a;
-                            lo[i] = b;
-                        }
+                        for (int e = 0; e < 4; ++e) v[e] = times * acc[t][4 * q + e];
+                        split(v, &hi, &lo);
                         *reinterpret_cast<h16x4*>(&sm[0][run_of(t, q)]) = hi;
                         *reinterpret_cast<h16x4*>(&sm[1][run_of(t, q)]) = lo;
                     }
@@ -603,7 +616,7 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             acc[t][4 * q + i] =
-                                fmaf(own, join(hi[i], lo[i]), times * acc[t][4 * q + i]);
+                                add_own(own, hi[i], lo[i], times * acc[t][4 * q + i]);
                     }
         }
         __syncthreads();
@@ -620,14 +633,18 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float v = fmaf(own, join(xh[t][i / 8][i % 8], xl[t][i / 8][i % 8]),
-                                     times * acc[t][i]);
-                acc[t][i] = ldexpf(v, last ? -e : 0);
-                h16 hi, lo;
-                split(v, &hi, &lo);
-                xh[t][i / 8][i % 8] = hi;
-                xl[t][i / 8][i % 8] = lo;
+            for (int q = 0; q < 4; ++q) {
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int x = 4 * (q & 1) + i;
+                    v[i] = add_own(own, xh[t][q / 2][x], xl[t][q / 2][x], times * acc[t][4 * q + i]);
+                }
+                if (last)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[t][4 * q + i] = ldexpf(v[i] * kUnscale, -e);
+                else
+                    keep(t, q, v);
             }
     }
     if (steps == 0) {
