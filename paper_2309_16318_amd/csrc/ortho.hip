@@ -449,29 +449,34 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
 // columns in LDS in that order, and their symmetry lets a lane write its column
 // as a row, four elements at once.  X goes to LDS by rows for the Gram product
 // only, then A, then B take its place.
-template <int P, int DT>
+// RT = ceil(k / 32) row tiles are in use: known to the compiler, so that nothing
+// between the instructions asks whether one is, and symmetric products are
+// computed by half (1024 matrices of 128 x 128: 191 us without either, 187
+// without the second, 165).
+template <int P, int RT, int DT>
 __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out, int m, int n,
                                                         int steps, float ca, float cb, float cc,
                                                         float eps, float rate) {
     constexpr int NT = P / 32, PITCH = P + 8;  // a row's 16 bytes more spread the banks
-    __shared__ __attribute__((aligned(16))) h16 sm[2][P * PITCH];
+    __shared__ __attribute__((aligned(16))) h16 sm[2][32 * RT * PITCH];
     __shared__ float red[2][NT];
     const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // The second workgroup of a CU (256 of them) counts its waves from the other
+    // half: the first half of them has more to do, and they share the SIMDs.
+    const int wave = (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) +
+                      (blockIdx.x >> 8 & 1) * (NT / 2)) % NT;
     const int r32 = lane & 31, half = lane >> 5;
     const bool tall = m > n;
     const int k = tall ? n : m, r = tall ? m : n;
-    const int rt = (k + 31) / 32;               // row tiles in use
-    const int ks = (k + 15) / 16, rs = (r + 15) / 16;
     const int col = 32 * wave + r32;
     const long long base = (long long)blockIdx.x * m * n;
     auto row_of = [&](int t, int q, int e) { return 32 * t + 8 * q + 4 * half + e; };
     auto at_of = [&](int row) { return base + (tall ? (long long)col * n + row : (long long)row * n + col); };
 
-    f32x16 acc[NT];
+    f32x16 acc[RT];
     float top = 0.f, bad = 0.f;
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int row = row_of(t, i / 4, i % 4);
@@ -491,7 +496,7 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
     float sum = 0.f;
     if (top > 0.f)
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < RT; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 acc[t][i] /= top;
@@ -510,7 +515,7 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
         depth = log2f(den / norm);
     }
     inv = ldexpf(inv, shift_of(depth, 0.f, 0));
-    h16x8 xh[NT][2], xl[NT][2];
+    h16x8 xh[RT][2], xl[RT][2];
     // X's parts from four values times kScale
     auto keep = [&](int t, int q, const float (&v)[4]) {
         h16x4 hi, lo;
@@ -522,7 +527,7 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
         }
     };
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             float v[4];
@@ -531,31 +536,44 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
             keep(t, q, v);
         }
 
-    // acc = sum over `count` steps of 16 of rows (32 t ..) of LDS against `right`
-    auto product = [&](int count, auto&& right) {
+    // acc[d] = sum over K steps of 16 of the rows of tile tile_of(d) of LDS
+    // against `right`, d < D
+    auto product = [&](auto D, auto K, auto&& tile_of, auto&& right) {
+        constexpr int N = decltype(D)::value;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) acc[t] = f32x16{};
+        for (int d = 0; d < N; ++d) acc[d] = f32x16{};
 #pragma unroll
-        for (int s = 0; s < P / 16; ++s) {
-            if (s >= count) break;
-            h16x8 b[2], a[NT][2];
+        for (int s = 0; s < decltype(K)::value; ++s) {
+            h16x8 b[2], a[N][2];
             right(s, b);
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-                if (t < rt)
+            for (int d = 0; d < N; ++d)
 #pragma unroll
-                    for (int p = 0; p < 2; ++p)
-                        a[t][p] = *reinterpret_cast<const h16x8*>(
-                            &sm[p][(32 * t + r32) * PITCH + 16 * s + 8 * half]);
+                for (int p = 0; p < 2; ++p)
+                    a[d][p] = *reinterpret_cast<const h16x8*>(
+                        &sm[p][(32 * tile_of(d) + r32) * PITCH + 16 * s + 8 * half]);
 #pragma unroll
             for (int p = 0; p < 3; ++p)
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
-                    if (t < rt)
-                        acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                            a[t][p == 0], b[p == 1], acc[t], 0, 0, 0);
+                for (int d = 0; d < N; ++d)
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[d][p == 0], b[p == 1],
+                                                                    acc[d], 0, 0, 0);
         }
     };
+    // The tiles of a symmetric product that a wave below RT computes: those of its
+    // column from the diagonal one on, going round, half of them in all (the one
+    // half way round by the first half of the waves); it writes each twice.
+    constexpr int HALF = RT / 2 + 1, SURE = (RT + 1) / 2;
+    auto across = [&](int d) { return (wave + d) % RT; };
+    auto mine = [&](int d) { return d < SURE || wave < RT / 2; };
+    auto symmetric = [&](auto K, auto&& right) {
+        if (HALF == SURE || wave < RT / 2)
+            product(std::integral_constant<int, HALF>{}, K, across, right);
+        else
+            product(std::integral_constant<int, SURE>{}, K, across, right);
+    };
+    constexpr std::integral_constant<int, 2 * RT> kRows{};
+    constexpr std::integral_constant<int, P / 16> kCols{};
     // the wave's 32 rows of LDS as the right operand
     auto own_rows = [&](int s, h16x8 (&b)[2]) {
 #pragma unroll
@@ -570,68 +588,77 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
     const float f = kUnscale;  // of a product, for a value times kScale
     for (int s = 0; s < steps; ++s) {
         const int e = shift_of(depth, rate, s);
-        const bool square = 32 * wave < k, wide = 32 * wave < r;
+        const bool square = wave < RT;
         if (s > 0) __syncthreads();  // B has been read
-        if (wide)
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-                if (t < rt)
+        for (int t = 0; t < RT; ++t)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int at = row_of(t, q, lane & 3) * PITCH + (col & ~3);
-                        const h16x8 h = xh[t][q / 2], l = xl[t][q / 2];
-                        *reinterpret_cast<h16x4*>(&sm[0][at]) = quad_turn(q & 1 ? h.hi : h.lo);
-                        *reinterpret_cast<h16x4*>(&sm[1][at]) = quad_turn(q & 1 ? l.hi : l.lo);
-                    }
+            for (int q = 0; q < 4; ++q) {
+                const int at = row_of(t, q, lane & 3) * PITCH + (col & ~3);
+                const h16x8 h = xh[t][q / 2], l = xl[t][q / 2];
+                *reinterpret_cast<h16x4*>(&sm[0][at]) = quad_turn(q & 1 ? h.hi : h.lo);
+                *reinterpret_cast<h16x4*>(&sm[1][at]) = quad_turn(q & 1 ? l.hi : l.lo);
+            }
         __syncthreads();
-        if (square) product(rs, own_rows);
+        if (square) symmetric(kCols, own_rows);
         __syncthreads();
         auto put = [&](float times) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-                if (t < rt)
+            for (int d = 0; d < HALF; ++d)
+                if (mine(d)) {
+                    const int t = across(d);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         h16x4 hi, lo;
                         float v[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = times * acc[t][4 * q + e];
+                        for (int e = 0; e < 4; ++e) v[e] = times * acc[d][4 * q + e];
                         split(v, &hi, &lo);
                         *reinterpret_cast<h16x4*>(&sm[0][run_of(t, q)]) = hi;
                         *reinterpret_cast<h16x4*>(&sm[1][run_of(t, q)]) = lo;
+                        if (d > 0) {
+                            // run c of its 16 columns sits at 0, 2, 1, 3
+                            const int c = (r32 >> 2) & 3;
+                            const int at = row_of(t, q, lane & 3) * PITCH + 32 * wave +
+                                           16 * (r32 >> 4) + 4 * (2 * (c & 1) + (c >> 1));
+                            *reinterpret_cast<h16x4*>(&sm[0][at]) = quad_turn(hi);
+                            *reinterpret_cast<h16x4*>(&sm[1][at]) = quad_turn(lo);
+                        }
                     }
+                }
         };
         if (square) put(f);  // A
         __syncthreads();
         if (square) {
-            product(ks, own_rows);
+            symmetric(kRows, own_rows);
             const float own = ldexpf(cb, -2 * e), times = ldexpf(cc * f, -4 * e);
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-                if (t < rt)
+            for (int d = 0; d < HALF; ++d)
+                if (mine(d))
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const h16x4 hi = *reinterpret_cast<const h16x4*>(&sm[0][run_of(t, q)]);
-                        const h16x4 lo = *reinterpret_cast<const h16x4*>(&sm[1][run_of(t, q)]);
+                        const int at = run_of(across(d), q);
+                        const h16x4 hi = *reinterpret_cast<const h16x4*>(&sm[0][at]);
+                        const h16x4 lo = *reinterpret_cast<const h16x4*>(&sm[1][at]);
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            acc[t][4 * q + i] =
-                                add_own(own, hi[i], lo[i], times * acc[t][4 * q + i]);
+                            acc[d][4 * q + i] =
+                                add_own(own, hi[i], lo[i], times * acc[d][4 * q + i]);
                     }
         }
         __syncthreads();
         if (square) put(1.f);  // B
         __syncthreads();
-        if (!wide) continue;
-        product(ks, [&](int c, h16x8 (&b)[2]) {
-            b[0] = xh[c / 2][c % 2];
-            b[1] = xl[c / 2][c % 2];
-        });
+        product(std::integral_constant<int, RT>{}, kRows, [](int d) { return d; },
+                [&](int c, h16x8 (&b)[2]) {
+                    b[0] = xh[c / 2][c % 2];
+                    b[1] = xl[c / 2][c % 2];
+                });
         const bool last = s + 1 == steps;
         const int d = last ? 0 : shift_of(depth, rate, s + 1) - e;
         const float own = ldexpf(ca, d), times = ldexpf(f, d);
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < RT; ++t)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 float v[4];
@@ -650,12 +677,12 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
     if (steps == 0) {
         const int e = shift_of(depth, 0.f, 0);
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < RT; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[t][i] = ldexpf(acc[t][i], -e);
     }
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int row = row_of(t, i / 4, i % 4);
@@ -715,12 +742,24 @@ hipError_t run_small(const void* G, void* X, int N, int m, int n, int steps, flo
         const unsigned some = (unsigned)std::min<long long>(1 << 23, N - at);
         const void* g = (const char*)G + at * sz;
         void* x = (char*)X + at * sz;
-        if (side <= 32)
-            ortho_small<32, DT><<<some, 64, 0, st>>>(g, x, m, n, steps, ca, cb, cc, eps, rate);
-        else if (side <= 64)
-            ortho_small<64, DT><<<some, 128, 0, st>>>(g, x, m, n, steps, ca, cb, cc, eps, rate);
-        else
-            ortho_small<128, DT><<<some, 256, 0, st>>>(g, x, m, n, steps, ca, cb, cc, eps, rate);
+        auto go = [&](auto p, auto rt) {
+            constexpr int P = decltype(p)::value, RT = decltype(rt)::value;
+            ortho_small<P, RT, DT><<<some, 2 * P, 0, st>>>(g, x, m, n, steps, ca, cb, cc, eps, rate);
+        };
+        constexpr std::integral_constant<int, 1> one{};
+        constexpr std::integral_constant<int, 2> two{};
+        constexpr std::integral_constant<int, 3> three{};
+        constexpr std::integral_constant<int, 4> four{};
+        const int rt = (std::min(m, n) + 31) / 32;
+        if (side <= 32) {
+            go(std::integral_constant<int, 32>{}, one);
+        } else if (side <= 64) {
+            constexpr std::integral_constant<int, 64> p{};
+            rt == 1 ? go(p, one) : go(p, two);
+        } else {
+            constexpr std::integral_constant<int, 128> p{};
+            rt == 1 ? go(p, one) : rt == 2 ? go(p, two) : rt == 3 ? go(p, three) : go(p, four);
+        }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
