@@ -32,19 +32,22 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kScale = 1024.f, kUnscale = 1.f / 1024.f;  // 2^10
 
-// The parts of four values that are already multiplied by kScale: two packed
-// conversions and two mixed-precision multiply-adds a pair (the matrix cores
+// The NP parts of four values that are already multiplied by kScale: a packed
+// conversion and a mixed-precision multiply-add each a pair (the matrix cores
 // and these instructions share a wave's issue slots).
-__device__ __forceinline__ void split(const float (&s)[4], h16x4* hi, h16x4* lo) {
+template <int NP>
+__device__ __forceinline__ void split(const float (&s)[4], h16x4 (&part)[NP]) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
     typedef h16 h16x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
     for (int i = 0; i < 4; i += 2) {
-        const h16x2 h = __builtin_convertvector((f32x2{s[i], s[i + 1]}), h16x2);
-        const f32x2 r{fmaf((float)h.x, -1.f, s[i]), fmaf((float)h.y, -1.f, s[i + 1])};
-        const h16x2 l = __builtin_convertvector(r, h16x2);
-        (*hi)[i] = h.x, (*hi)[i + 1] = h.y;
-        (*lo)[i] = l.x, (*lo)[i + 1] = l.y;
+        f32x2 r{s[i], s[i + 1]};
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const h16x2 h = __builtin_convertvector(r, h16x2);
+            part[p][i] = h.x, part[p][i + 1] = h.y;
+            r = f32x2{fmaf((float)h.x, -1.f, r.x), fmaf((float)h.y, -1.f, r.y)};
+        }
     }
 }
 // own (hi + lo) + v
@@ -212,14 +215,14 @@ __global__ void __launch_bounds__(256) ortho_start(const void* G, Panels X, cons
     // four elements of a row
     for (int e = threadIdx.x; e < 64 * 16; e += 256) {
         const int i = e / 16, j = e % 16 * 4;
-        h16x4 hi, lo;
+        h16x4 x[2];
         float v[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) v[u] = kScale * (tall ? t[j + u][i] : t[i][j + u]);
-        split(v, &hi, &lo);
+        split(v, x);
         h16* p = tall ? X.at(z, j0 + i, i0 + j) : X.at(z, i0 + i, j0 + j);
-        *reinterpret_cast<h16x4*>(p) = hi;
-        *reinterpret_cast<h16x4*>(p + kLo) = lo;
+        *reinterpret_cast<h16x4*>(p) = x[0];
+        *reinterpret_cast<h16x4*>(p + kLo) = x[1];
     }
 }
 
@@ -421,7 +424,12 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
                                     g.out, (z * g.m + r) * (long long)g.n + c, one);
                         }
                     }
-                    if (OUT < 0) split(v, &hi[u], &lo[u]);
+                    if constexpr (OUT < 0) {
+                        h16x4 x[2];
+                        split(v, x);
+                        hi[u] = x[0];
+                        lo[u] = x[1];
+                    }
                     if (OUT < 0 && (MODE == APPLY || bi != bj)) {
                         h16* c = g.C.at(z, row + (lane & 3), col & ~3);
                         *reinterpret_cast<h16x4*>(c) = quad_turn(hi[u]);
@@ -449,6 +457,114 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
 // columns in LDS in that order, and their symmetry lets a lane write its column
 // as a row, four elements at once.  X goes to LDS by rows for the Gram product
 // only, then A, then B take its place.
+// 1 / (|G| + eps), shifted for the first step, for a matrix whose elements have
+// been divided by the largest, `top`, and then have the square sum `sum`; a zero
+// matrix stays zero, whatever eps, and NaN stays NaN.
+__device__ __forceinline__ float inverse_norm(float top, float sum, float eps, float* depth) {
+    *depth = 0.f;
+    if (!(top > 0.f)) return sum == sum ? 0.f : sum;
+    const float norm = sqrtf(sum), den = norm + eps / top;
+    *depth = log2f(den / norm);
+    return ldexpf(1.f / den, shift_of(*depth, 0.f, 0));
+}
+
+// A matrix of up to 16 x 16 in one wave's registers: element e of a lane is row
+// 4 (lane / 16) + e of column lane % 16, which is how a product leaves a tile and
+// how the next one takes its right operand, and by the symmetry of A and B its
+// left one.  X is turned for the Gram product by lane exchanges.  Three parts to
+// a value, six terms to a product (as P = 32 below).  In the 32 x 32 kernel 1024
+// matrices of 16 x 16 took 12.4 us, 9.0 here (a call).
+template <int DT>
+__global__ void __launch_bounds__(64) ortho_tiny(const void* G, void* out, int m, int n, int steps,
+                                                 float ca, float cb, float cc, float eps,
+                                                 float rate) {
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    constexpr int NP = 3;
+    const int lane = threadIdx.x, col = lane & 15, row0 = lane >> 4 << 2;
+    const bool tall = m > n;
+    const int k = tall ? n : m, r = tall ? m : n;
+    const long long base = (long long)blockIdx.x * m * n;
+    auto at_of = [&](int row) { return base + (tall ? (long long)col * n + row : (long long)row * n + col); };
+    float v[4];
+    float top = 0.f, bad = 0.f, sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[e] = row0 + e < k && col < r ? (float)pack_load<DT, 1>(G, at_of(row0 + e)).e[0] : 0.f;
+        top = fmaxf(top, fabsf(v[e]));
+        bad += v[e] * 0.f;  // NaN where an element is not finite
+    }
+    for (int s = 1; s < 64; s *= 2) {
+        top = fmaxf(top, __shfl_xor(top, s));
+        bad += __shfl_xor(bad, s);
+    }
+    if (top > 0.f)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] /= top;
+            sum = fmaf(v[e], v[e], sum);
+        }
+    for (int s = 1; s < 64; s *= 2) sum += __shfl_xor(sum, s);
+    float depth;
+    const float inv = inverse_norm(top, sum + bad, eps, &depth);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] *= inv * kScale;
+    h16x4 x[NP];
+    split(v, x);
+    // lane 16 i + 4 j + l of a quad_turn'ed tile holds row 4 i + l, columns 4 j ..:
+    // lane 16 j + 4 i + l is to have it
+    const int from = (16 * (col >> 2) + 4 * (lane >> 4) + (col & 3)) * 4;
+    auto turned = [&](h16x4 a) {
+        typedef int i32x2 __attribute__((ext_vector_type(2)));
+        const i32x2 w = __builtin_bit_cast(i32x2, quad_turn(a));
+        return __builtin_bit_cast(h16x4, i32x2{__builtin_amdgcn_ds_bpermute(from, w.x),
+                                               __builtin_amdgcn_ds_bpermute(from, w.y)});
+    };
+    auto product = [&](const h16x4 (&l)[NP], const h16x4 (&r)[NP]) {
+        f32x4 a[2] = {};  // small terms, and hi hi
+#pragma unroll
+        for (int order = NP - 1; order >= 0; --order)
+#pragma unroll
+            for (int p = order; p >= 0; --p)
+                a[order == 0] = __builtin_amdgcn_mfma_f32_16x16x16f16(l[p], r[order - p],
+                                                                      a[order == 0], 0, 0, 0);
+        return a[0] + a[1];
+    };
+    auto parts = [&](const f32x4& a, h16x4 (&to)[NP]) {
+        const float s[4] = {a.x, a.y, a.z, a.w};
+        split(s, to);
+    };
+    const float f = kUnscale;
+    for (int s = 0; s < steps; ++s) {
+        const int e = shift_of(depth, rate, s);
+        h16x4 y[NP];
+#pragma unroll
+        for (int p = 0; p < NP; ++p) y[p] = turned(x[p]);
+        const f32x4 A = product(y, y) * f;
+        parts(A, y);
+        const f32x4 B = A * ldexpf(cb, -2 * e) + product(y, y) * ldexpf(cc * f, -4 * e);
+        parts(B, y);
+        const bool last = s + 1 == steps;
+        const int d = last ? 0 : shift_of(depth, rate, s + 1) - e;
+        f32x4 c = product(y, x) * ldexpf(f, d);
+        const float own = ldexpf(ca, d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int p = NP - 1; p >= 0; --p) c[i] = fmaf((float)x[p][i], own, c[i]);
+            v[i] = last ? ldexpf(c[i], -e) : c[i];
+        }
+        split(v, x);
+    }
+    if (steps == 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = ldexpf(v[i], -shift_of(depth, 0.f, 0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float one[1] = {v[i] * kUnscale};
+        if (row0 + i < k && col < r) pack_store<DT, 1>(out, at_of(row0 + i), one);
+    }
+}
+
 // RT = ceil(k / 32) row tiles are in use: known to the compiler, so that nothing
 // between the instructions asks whether one is, and symmetric products are
 // computed by half (1024 matrices of 128 x 128: 191 us without either, 187
@@ -458,7 +574,11 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
                                                         int steps, float ca, float cb, float cc,
                                                         float eps, float rate) {
     constexpr int NT = P / 32, PITCH = P + 8;  // a row's 16 bytes more spread the banks
-    __shared__ __attribute__((aligned(16))) h16 sm[2][32 * RT * PITCH];
+    // Sums of few products have no rounding of their own to hide two parts' in
+    // (4 x 4 matrices erred by 1.5 times what float32 products do, 11 x 11 by up
+    // to 1.7): there a value has three parts, all its bits, and a product six terms.
+    constexpr int NP = P == 32 ? 3 : 2;
+    __shared__ __attribute__((aligned(16))) h16 sm[NP][32 * RT * PITCH];
     __shared__ float red[2][NT];
     const int lane = threadIdx.x & 63;
     // The second workgroup of a CU (256 of them) counts its waves from the other
@@ -507,24 +627,17 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
     __syncthreads();
     sum = bad;
     for (int v = 0; v < NT; ++v) sum += red[0][v];
-    // a zero matrix stays zero, whatever eps; NaN stays NaN
-    float depth = 0.f, inv = sum == sum ? 0.f : sum;
-    if (top > 0.f) {
-        const float norm = sqrtf(sum), den = norm + eps / top;
-        inv = 1.f / den;
-        depth = log2f(den / norm);
-    }
-    inv = ldexpf(inv, shift_of(depth, 0.f, 0));
-    h16x8 xh[RT][2], xl[RT][2];
+    float depth;
+    const float inv = inverse_norm(top, sum, eps, &depth);
+    h16x8 x[RT][2][NP];
     // X's parts from four values times kScale
     auto keep = [&](int t, int q, const float (&v)[4]) {
-        h16x4 hi, lo;
-        split(v, &hi, &lo);
+        h16x4 part[NP];
+        split(v, part);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            xh[t][q / 2][4 * (q & 1) + e] = hi[e];
-            xl[t][q / 2][4 * (q & 1) + e] = lo[e];
-        }
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[t][q / 2][p][4 * (q & 1) + e] = part[p][e];
     };
 #pragma unroll
     for (int t = 0; t < RT; ++t)
@@ -544,20 +657,22 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
         for (int d = 0; d < N; ++d) acc[d] = f32x16{};
 #pragma unroll
         for (int s = 0; s < decltype(K)::value; ++s) {
-            h16x8 b[2], a[N][2];
+            h16x8 b[NP], a[N][NP];
             right(s, b);
 #pragma unroll
             for (int d = 0; d < N; ++d)
 #pragma unroll
-                for (int p = 0; p < 2; ++p)
+                for (int p = 0; p < NP; ++p)
                     a[d][p] = *reinterpret_cast<const h16x8*>(
                         &sm[p][(32 * tile_of(d) + r32) * PITCH + 16 * s + 8 * half]);
 #pragma unroll
-            for (int p = 0; p < 3; ++p)
+            for (int order = NP - 1; order >= 0; --order)  // the small terms first
 #pragma unroll
-                for (int d = 0; d < N; ++d)
-                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[d][p == 0], b[p == 1],
-                                                                    acc[d], 0, 0, 0);
+                for (int p = order; p >= 0; --p)
+#pragma unroll
+                    for (int d = 0; d < N; ++d)
+                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[d][p], b[order - p],
+                                                                        acc[d], 0, 0, 0);
         }
     };
     // The tiles of a symmetric product that a wave below RT computes: those of its
@@ -575,9 +690,9 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
     constexpr std::integral_constant<int, 2 * RT> kRows{};
     constexpr std::integral_constant<int, P / 16> kCols{};
     // the wave's 32 rows of LDS as the right operand
-    auto own_rows = [&](int s, h16x8 (&b)[2]) {
+    auto own_rows = [&](int s, h16x8 (&b)[NP]) {
 #pragma unroll
-        for (int p = 0; p < 2; ++p)
+        for (int p = 0; p < NP; ++p)
             b[p] = *reinterpret_cast<const h16x8*>(&sm[p][col * PITCH + 16 * s + 8 * half]);
     };
     // rows 8 q + 4 half + 0 .. 3 of tile t of the lane's column, by symmetry
@@ -586,8 +701,77 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
         return col * PITCH + 32 * t + 16 * (q >> 1) + 4 * (2 * half + (q & 1));
     };
     const float f = kUnscale;  // of a product, for a value times kScale
+    // One tile, one wave: A and B are symmetric, so that a lane's column, as a
+    // product leaves it, is its row as the left operand too: they never leave the
+    // registers.  X crosses LDS for the Gram product.
+    auto one_tile = [&](int s, int e) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                const h16x8 h = x[0][q / 2][p];
+                *reinterpret_cast<h16x4*>(&sm[p][row_of(0, q, lane & 3) * PITCH + (col & ~3)]) =
+                    quad_turn(q & 1 ? h.hi : h.lo);
+            }
+        wave_sync();
+        h16x8 rows[2][NP];
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+                rows[c][p] = *reinterpret_cast<const h16x8*>(&sm[p][r32 * PITCH + 16 * c + 8 * half]);
+        wave_sync();
+        // two accumulators: a product need not wait for the one before it
+        auto times_of = [&](const h16x8 (&l)[2][NP], const h16x8 (&r)[2][NP]) {
+            f32x16 sum[2] = {};
+#pragma unroll
+            for (int order = NP - 1; order >= 0; --order)
+#pragma unroll
+                for (int p = order; p >= 0; --p)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        sum[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[c][p], r[c][order - p],
+                                                                        sum[c], 0, 0, 0);
+            return sum[0] + sum[1];
+        };
+        auto parts_of = [&](const f32x16& a, h16x8 (&to)[2][NP]) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float v[4] = {a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
+                h16x4 part[NP];
+                split(v, part);
+#pragma unroll
+                for (int p = 0; p < NP; ++p)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) to[q / 2][p][4 * (q & 1) + i] = part[p][i];
+            }
+        };
+        const bool last = s + 1 == steps;
+        const int d = last ? 0 : shift_of(depth, rate, s + 1) - e;
+        h16x8 y[2][NP];
+        const f32x16 A = times_of(rows, rows) * f;
+        parts_of(A, y);
+        const f32x16 B = A * ldexpf(cb, -2 * e) + times_of(y, y) * ldexpf(cc * f, -4 * e);
+        parts_of(B, y);
+        f32x16 v = times_of(y, x[0]) * ldexpf(f, d);
+        const float own = ldexpf(ca, d);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int p = NP - 1; p >= 0; --p)
+                v[i] = fmaf((float)x[0][i / 8][p][i % 8], own, v[i]);
+        if (last)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[0][i] = ldexpf(v[i] * kUnscale, -e);
+        else
+            parts_of(v, x[0]);
+    };
     for (int s = 0; s < steps; ++s) {
         const int e = shift_of(depth, rate, s);
+        if constexpr (NT == 1) {
+            one_tile(s, e);
+            continue;
+        }
         const bool square = wave < RT;
         if (s > 0) __syncthreads();  // B has been read
 #pragma unroll
@@ -595,9 +779,11 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int at = row_of(t, q, lane & 3) * PITCH + (col & ~3);
-                const h16x8 h = xh[t][q / 2], l = xl[t][q / 2];
-                *reinterpret_cast<h16x4*>(&sm[0][at]) = quad_turn(q & 1 ? h.hi : h.lo);
-                *reinterpret_cast<h16x4*>(&sm[1][at]) = quad_turn(q & 1 ? l.hi : l.lo);
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    const h16x8 h = x[t][q / 2][p];
+                    *reinterpret_cast<h16x4*>(&sm[p][at]) = quad_turn(q & 1 ? h.hi : h.lo);
+                }
             }
         __syncthreads();
         if (square) symmetric(kCols, own_rows);
@@ -609,20 +795,19 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
                     const int t = across(d);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        h16x4 hi, lo;
+                        h16x4 part[NP];
                         float v[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) v[e] = times * acc[d][4 * q + e];
-                        split(v, &hi, &lo);
-                        *reinterpret_cast<h16x4*>(&sm[0][run_of(t, q)]) = hi;
-                        *reinterpret_cast<h16x4*>(&sm[1][run_of(t, q)]) = lo;
-                        if (d > 0) {
-                            // run c of its 16 columns sits at 0, 2, 1, 3
-                            const int c = (r32 >> 2) & 3;
-                            const int at = row_of(t, q, lane & 3) * PITCH + 32 * wave +
-                                           16 * (r32 >> 4) + 4 * (2 * (c & 1) + (c >> 1));
-                            *reinterpret_cast<h16x4*>(&sm[0][at]) = quad_turn(hi);
-                            *reinterpret_cast<h16x4*>(&sm[1][at]) = quad_turn(lo);
+                        split(v, part);
+                        // run c of its 16 columns sits at 0, 2, 1, 3
+                        const int c = (r32 >> 2) & 3;
+                        const int at = row_of(t, q, lane & 3) * PITCH + 32 * wave +
+                                       16 * (r32 >> 4) + 4 * (2 * (c & 1) + (c >> 1));
+#pragma unroll
+                        for (int p = 0; p < NP; ++p) {
+                            *reinterpret_cast<h16x4*>(&sm[p][run_of(t, q)]) = part[p];
+                            if (d > 0) *reinterpret_cast<h16x4*>(&sm[p][at]) = quad_turn(part[p]);
                         }
                     }
                 }
@@ -638,21 +823,24 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const int at = run_of(across(d), q);
-                        const h16x4 hi = *reinterpret_cast<const h16x4*>(&sm[0][at]);
-                        const h16x4 lo = *reinterpret_cast<const h16x4*>(&sm[1][at]);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            acc[d][4 * q + i] =
-                                add_own(own, hi[i], lo[i], times * acc[d][4 * q + i]);
+                        for (int i = 0; i < 4; ++i) acc[d][4 * q + i] *= times;
+#pragma unroll
+                        for (int p = NP - 1; p >= 0; --p) {
+                            const h16x4 part = *reinterpret_cast<const h16x4*>(&sm[p][at]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                acc[d][4 * q + i] = fmaf((float)part[i], own, acc[d][4 * q + i]);
+                        }
                     }
         }
         __syncthreads();
         if (square) put(1.f);  // B
         __syncthreads();
         product(std::integral_constant<int, RT>{}, kRows, [](int d) { return d; },
-                [&](int c, h16x8 (&b)[2]) {
-                    b[0] = xh[c / 2][c % 2];
-                    b[1] = xl[c / 2][c % 2];
+                [&](int c, h16x8 (&b)[NP]) {
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) b[p] = x[c / 2][c % 2][p];
                 });
         const bool last = s + 1 == steps;
         const int d = last ? 0 : shift_of(depth, rate, s + 1) - e;
@@ -664,8 +852,10 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
                 float v[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int x = 4 * (q & 1) + i;
-                    v[i] = add_own(own, xh[t][q / 2][x], xl[t][q / 2][x], times * acc[t][4 * q + i]);
+                    v[i] = times * acc[t][4 * q + i];
+#pragma unroll
+                    for (int p = NP - 1; p >= 0; --p)
+                        v[i] = fmaf((float)x[t][q / 2][p][4 * (q & 1) + i], own, v[i]);
                 }
                 if (last)
 #pragma unroll
@@ -751,7 +941,9 @@ hipError_t run_small(const void* G, void* X, int N, int m, int n, int steps, flo
         constexpr std::integral_constant<int, 3> three{};
         constexpr std::integral_constant<int, 4> four{};
         const int rt = (std::min(m, n) + 31) / 32;
-        if (side <= 32) {
+        if (side <= 16) {
+            ortho_tiny<DT><<<some, 64, 0, st>>>(g, x, m, n, steps, ca, cb, cc, eps, rate);
+        } else if (side <= 32) {
             go(std::integral_constant<int, 32>{}, one);
         } else if (side <= 64) {
             constexpr std::integral_constant<int, 64> p{};
