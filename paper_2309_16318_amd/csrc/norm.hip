@@ -85,6 +85,33 @@ struct Cols {
     }
 };
 
+// v + v of the lane that the step pairs this one with: inside 16 lanes by lane
+// permutations of the add itself (pairs, quads, then the mirrored half and row),
+// beyond by exchanging rows and halves of the wave; no LDS round trips.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+    return v + __int_as_float(
+                   __builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
+}
+// The sum over the G (a power of two) consecutive lanes of a row.
+__device__ __forceinline__ float lanes_sum(float v, int G) {
+    if (G > 1) v = dpp_add<0xB1>(v);
+    if (G > 2) v = dpp_add<0x4E>(v);
+    if (G > 4) v = dpp_add<0x141>(v);
+    if (G > 8) v = dpp_add<0x140>(v);
+    if (G > 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v),
+                                                        false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (G > 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v),
+                                                        false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    return v;
+}
+
 // Sums of N values over the threads of a row, in every one of them.
 template <int N, bool BIG>
 struct RowSum {
@@ -92,14 +119,11 @@ struct RowSum {
     int G, turn = 0;
     __device__ __forceinline__ void operator()(float (&v)[N]) {
         if constexpr (!BIG) {
-            for (int m = 1; m < G; m *= 2)
 #pragma unroll
-                for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], m);
+            for (int i = 0; i < N; ++i) v[i] = lanes_sum(v[i], G);
         } else {
 #pragma unroll
-            for (int m = 1; m < 64; m *= 2)
-#pragma unroll
-                for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], m);
+            for (int i = 0; i < N; ++i) v[i] = lanes_sum(v[i], 64);
             // two buffers in turn: a wave may be one sum ahead of another
             if ((threadIdx.x & 63) == 0)
 #pragma unroll
@@ -154,12 +178,6 @@ __global__ void __launch_bounds__(MAXT ? MAXT : kSmallWG) norm_fwd(NormArgs k, i
     const Place<BIG> me(G);
     const Cols<DT, VEC> cols(me.t, G, k.w);
     RowSum<1, BIG> sum{sm, G};
-    float kw[E], pre[E];
-    cols.weights(k.w_post, 1.f, kw);
-    cols.weights(k.scale, 1.f, pre);
-#pragma unroll
-    for (int j = 0; j < E; ++j) kw[j] *= pre[j];
-    cols.weights(k.w_pre, 1.f, pre);
     const float inv = 1.f / (float)k.w;
     const long long rows = (long long)k.B * k.L;
     const long long step = (long long)gridDim.x * me.subs;
@@ -173,8 +191,15 @@ __global__ void __launch_bounds__(MAXT ? MAXT : kSmallWG) norm_fwd(NormArgs k, i
         if (k.y) cols.hold(k.y, r * k.ldy, q.y);
         if (k.gate) cols.hold(k.z, (k.z_per_seq ? r / k.L : r) * k.ldz, q.z);
     };
+    // the first row is asked for before the weights
     const long long first = (long long)blockIdx.x * me.subs;
-    if (AHEAD && first < rows) fetch(first, next);
+    if (first < rows) fetch(first, AHEAD ? next : now);
+    float kw[E], pre[E];
+    cols.weights(k.w_post, 1.f, kw);
+    cols.weights(k.scale, 1.f, pre);
+#pragma unroll
+    for (int j = 0; j < E; ++j) kw[j] *= pre[j];
+    cols.weights(k.w_pre, 1.f, pre);
     // the same number of turns for all threads of the workgroup
     for (long long r0 = first; r0 < rows; r0 += step) {
         const bool live = r0 + me.sub < rows;
@@ -182,7 +207,7 @@ __global__ void __launch_bounds__(MAXT ? MAXT : kSmallWG) norm_fwd(NormArgs k, i
         if constexpr (AHEAD) {
             now = next;
             if (r0 + step < rows) fetch(r0 + step, next);
-        } else {
+        } else if (r0 != first) {
             fetch(r0, now);
         }
         float x[E];
@@ -238,12 +263,6 @@ __global__ void __launch_bounds__(MAXT ? MAXT : kSmallWG) norm_bwd(NormArgs k, i
     const Place<BIG> me(G);
     const Cols<DT, VEC> cols(me.t, G, k.w);
     RowSum<3, BIG> sum{sm, G};
-    float kw[E], pre[E];
-    cols.weights(k.w_post, 1.f, kw);
-    cols.weights(k.scale, 1.f, pre);
-#pragma unroll
-    for (int j = 0; j < E; ++j) kw[j] *= pre[j];
-    cols.weights(k.w_pre, 0.f, pre);
     const float inv = 1.f / (float)k.w;
     // with one gate per sequence `parts` workgroups share a sequence
     const long long rows = k.z_per_seq ? k.L : (long long)k.B * k.L;
@@ -269,18 +288,25 @@ __global__ void __launch_bounds__(MAXT ? MAXT : kSmallWG) norm_bwd(NormArgs k, i
         q.rp = k.w_post ? k.rstd_post[r] : 1.f;
         q.rq = k.w_pre ? k.rstd_pre[r] : 0.f;
     };
+    // the first row is asked for before the weights
+    fetch(b0, AHEAD ? next : now);
     float acc1[E] = {}, acc2[E] = {};
     float z[E] = {}, v[E], slope[E];
     if (k.gate && k.z_per_seq) cols.load(k.z, seq * k.ldz, z);
+    float kw[E], pre[E];
+    cols.weights(k.w_post, 1.f, kw);
+    cols.weights(k.scale, 1.f, pre);
+#pragma unroll
+    for (int j = 0; j < E; ++j) kw[j] *= pre[j];
+    cols.weights(k.w_pre, 0.f, pre);
     gate_values(k.gate, z, v, slope);
-    if (AHEAD) fetch(b0, next);
     for (long long r0 = b0; r0 < b1; r0 += me.subs) {
         const bool live = r0 + me.sub < b1;
         const long long r = live ? r0 + me.sub : b1 - 1;
         if constexpr (AHEAD) {
             now = next;
             if (r0 + me.subs < b1) fetch(r0 + me.subs, next);
-        } else {
+        } else if (r0 != b0) {
             fetch(r0, now);
         }
         if (row_gate) {
