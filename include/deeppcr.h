@@ -396,7 +396,7 @@ int deeppcr_seq_backward(const float* W, const float* bias, const float* z0, con
  * validation before any HIP call, no wait for the GPU, no overlap of an
  * output with another argument but where the text allows it, results that
  * are the same run to run.  Every launch is a kernel, so that each call can
- * sit in a captured graph.  B w <= 2^31 - 64 and L <= 2^30.
+ * sit in a captured graph.
  */
 enum { DEEPPCR_F32 = 0, DEEPPCR_BF16 = 1, DEEPPCR_F16 = 2 };
 enum {
@@ -428,8 +428,8 @@ enum {
  * multipliers, so a direct gate's products over consecutive rows have to stay
  * inside the float32 range (those of multipliers in [-1, 1] do; an underflow
  * to zero is one of theirs).
- * workspace_bytes >= deeppcr_gated_scan_workspace_bytes(B, L, w), which is 0
- * for invalid sizes.
+ * B w <= 2^29 and L <= 2^30; workspace_bytes >=
+ * deeppcr_gated_scan_workspace_bytes(B, L, w), which is 0 for invalid sizes.
  */
 size_t deeppcr_gated_scan_workspace_bytes(int B, int L, int w);
 int deeppcr_gated_scan_forward(const void* a, long long lda, const void* u, long long ldu,

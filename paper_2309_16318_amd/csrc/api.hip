@@ -1493,11 +1493,13 @@ namespace {
 
 int elem_size(int dtype) { return dtype == DEEPPCR_F32 ? 4 : 2; }
 
-// A launch has fewer than 2^32 threads, so the channels of a batch are limited
-// (and their count, rounded up to whole waves, stays an int, as rows do).
 bool seq_ok(int B, int L, int w, int dtype) {
-    return B >= 1 && L >= 1 && L <= (1 << 30) && w >= 1 && dtype >= DEEPPCR_F32 && dtype <= DEEPPCR_F16 &&
-           (double)B * w <= 2147483584.0 && (double)B * L * w * 4.0 < 9.0e18;
+    return B >= 1 && L >= 1 && w >= 1 && dtype >= DEEPPCR_F32 && dtype <= DEEPPCR_F16 &&
+           (double)B * L * w * 4.0 < 9.0e18;
+}
+// A scan has up to 8 threads per channel, and a launch fewer than 2^32.
+bool scan_ok(int B, int L, int w, int dtype) {
+    return seq_ok(B, L, w, dtype) && (double)B * w <= 536870912.0 && L <= (1 << 30);
 }
 
 // A sequence with a row stride starts at any element.
@@ -1595,7 +1597,7 @@ bool iterates_stay(int steps, double ca, double cb, double cc) {
 extern "C" {
 
 size_t deeppcr_gated_scan_workspace_bytes(int B, int L, int w) {
-    return seq_ok(B, L, w, DEEPPCR_F32) ? scan_workspace(B, L, w) : 0;
+    return scan_ok(B, L, w, DEEPPCR_F32) ? scan_workspace(B, L, w) : 0;
 }
 
 int deeppcr_gated_scan_forward(const void* a, long long lda, const void* u, long long ldu,
@@ -1603,7 +1605,7 @@ int deeppcr_gated_scan_forward(const void* a, long long lda, const void* u, long
                                int L, int w, int gate, int dtype, void* workspace,
                                size_t workspace_bytes, void* stream) {
     const SpanGuard span_guard;
-    if (!a || !u || !x || !workspace || !seq_ok(B, L, w, dtype)) return DEEPPCR_EINVAL;
+    if (!a || !u || !x || !workspace || !scan_ok(B, L, w, dtype)) return DEEPPCR_EINVAL;
     if (gate != DEEPPCR_GATE_DIRECT && gate != DEEPPCR_GATE_SIGMOID) return DEEPPCR_EINVAL;
     const int e = elem_size(dtype);
     if (!on_element({a, u}, e) || !aligned({x0, lengths, x, x_last, workspace}))
@@ -1644,7 +1646,7 @@ int deeppcr_gated_scan_backward(const void* a, long long lda, const void* u, lon
                                 int B, int L, int w, int gate, int dtype, void* workspace,
                                 size_t workspace_bytes, void* stream) {
     const SpanGuard span_guard;
-    if (!a || !x || !g || !da || !du || !workspace || !seq_ok(B, L, w, dtype))
+    if (!a || !x || !g || !da || !du || !workspace || !scan_ok(B, L, w, dtype))
         return DEEPPCR_EINVAL;
     if (gate != DEEPPCR_GATE_DIRECT && gate != DEEPPCR_GATE_SIGMOID) return DEEPPCR_EINVAL;
     if (gate == DEEPPCR_GATE_SIGMOID && !u) return DEEPPCR_EINVAL;
@@ -1695,7 +1697,7 @@ int deeppcr_gated_scan_step(const void* a, long long lda, const void* u, long lo
                             const float* state, float* state_out, void* x, int B, int w, int gate,
                             int dtype, void* stream) {
     const SpanGuard span_guard;
-    if (!a || !u || !state || !state_out || !seq_ok(B, 1, w, dtype)) return DEEPPCR_EINVAL;
+    if (!a || !u || !state || !state_out || !scan_ok(B, 1, w, dtype)) return DEEPPCR_EINVAL;
     if (gate != DEEPPCR_GATE_DIRECT && gate != DEEPPCR_GATE_SIGMOID) return DEEPPCR_EINVAL;
     const int e = elem_size(dtype);
     if (!on_element({a, u}, e) || !aligned({state, state_out, x})) return DEEPPCR_EINVAL;

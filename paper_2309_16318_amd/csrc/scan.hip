@@ -86,7 +86,12 @@ struct Board {
     unsigned* tickets;
 };
 constexpr int kApart = 32;       // words between two groups' tickets, a cache line
-constexpr int kMaxGroups = 512;  // as many as are worth splitting
+// Tiles run at once where there are more than kWalk of them to a sequence and at
+// most kMaxGroups groups.  Forward and backward of bfloat16, all at once against
+// one after the other: 128 groups of 16 tiles 162 us against 290, 256 of 16 287
+// and 325, 512 of 8 266 and 274, 1024 of 4 261 and 267, 512 of 2 69 and 63; of
+// float32 8 groups of 8 34 and 76, of 2 34 and 28, 64 of 4 (forward) 16 and 16.
+constexpr int kMaxGroups = 512, kWalk = 3;
 
 __global__ void __launch_bounds__(256) scan_clear(unsigned long long* p, long long n,
                                                   unsigned* tickets) {
@@ -307,18 +312,26 @@ __global__ void __launch_bounds__(64 * S, 4) scan_tile(ScanArgs k, Board bd, int
     }
 }
 
-template <int DT, int GATE>
+// V channels of a sequence per thread.
+template <int DT, int V, int GATE>
 __global__ void __launch_bounds__(256) scan_step(const void* a, long long lda, const void* u,
                                                  long long ldu, const float* state,
                                                  float* state_out, void* x, int B, int w) {
-    const long long f = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (f >= (long long)B * w) return;
-    const long long b = f / w, c = f % w;
-    float s, q;
-    gate_of<GATE>((float)pack_load<DT, 1>(a, b * lda + c).e[0], &s, &q);
-    float out[1] = {fmaf(s, state[f], q * (float)pack_load<DT, 1>(u, b * ldu + c).e[0])};
-    state_out[f] = out[0];
-    if (x) pack_store<DT, 1>(x, f, out);
+    const int f = blockIdx.x * 256 + threadIdx.x, cw = w / V;
+    if (f >= B * cw) return;
+    const int b = f / cw, c = (f - b * cw) * V;
+    const long long at = (long long)b * w + c;
+    const Pack<DT, V> pa = pack_load<DT, V>(a, b * lda + c), pu = pack_load<DT, V>(u, b * ldu + c);
+    const Pack<0, V> ps = pack_load<0, V>(state, at);
+    float out[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        float s, q;
+        gate_of<GATE>((float)pa.e[v], &s, &q);
+        out[v] = fmaf(s, ps.e[v], q * (float)pu.e[v]);
+    }
+    pack_store<0, V>(state_out, at, out);
+    if (x) pack_store<DT, V>(x, at, out);
 }
 
 template <int N>
@@ -339,9 +352,15 @@ hipError_t by_type(int dtype, int gate, F&& f) {
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 long long chunks_of(int L) { return ((long long)L + T - 1) / T; }
-// Pairs and states, 8 bytes per channel each.
+bool at_once(long long groups, long long chunks) {
+    return chunks > kWalk && groups <= kMaxGroups && groups * chunks < (1 << 22);
+}
+// Pairs and states, 8 bytes per channel each, if some packs' tiles run at once.
 size_t board_words(int B, int L, int w) {
-    const long long ch = chunks_of(L);
+    const long long ch = chunks_of(L), channels = (long long)B * w;
+    if (!at_once((channels + 63) / 64, ch) &&
+        !(w % 2 == 0 && at_once((channels / 2 + 63) / 64, ch)))
+        return 0;
     return ((size_t)(ch + ch / kSuper) * B * w + 1) / 2 * 2;
 }
 
@@ -356,7 +375,7 @@ template <int DT, int V, int GATE, bool BWD>
 hipError_t tiles(const ScanArgs& k, hipStream_t st) {
     const long long F = (long long)k.B * (k.w / V), groups = (F + 63) / 64;
     const long long chunks = chunks_of(k.L);
-    if (chunks > 1 && groups <= kMaxGroups && groups * chunks < (1 << 22)) {
+    if (at_once(groups, chunks)) {
         Board bd;
         bd.tickets = (unsigned*)k.ws;
         bd.pairs = (unsigned long long*)((char*)k.ws + kMaxGroups * kApart * 4);
@@ -394,10 +413,22 @@ hipError_t launch_scan(bool bwd, const ScanArgs& k, int gate, int dtype, hipStre
 hipError_t launch_scan_step(const void* a, long long lda, const void* u, long long ldu,
                             const float* state, float* state_out, void* x, int B, int w, int gate,
                             int dtype, hipStream_t st) {
-    const unsigned grid = (unsigned)(((long long)B * w + 255) / 256);
+    // packs of 4 where the rows allow it, and there are threads enough without
+    ScanArgs k{};
+    k.a = a;
+    k.u = u;
+    k.lda = lda;
+    k.ldu = ldu;
+    k.w = w;
+    const bool packs = (long long)B * w >= 4 * 256 * 256 && in_packs(k, dtype, 4);
+    const long long n = (long long)B * (packs ? w / 4 : w);
+    const unsigned grid = (unsigned)((n + 255) / 256);
     return by_type(dtype, gate, [&](auto dt, auto gt) {
         constexpr int DT = decltype(dt)::value, GATE = decltype(gt)::value;
-        scan_step<DT, GATE><<<grid, 256, 0, st>>>(a, lda, u, ldu, state, state_out, x, B, w);
+        if (packs)
+            scan_step<DT, 4, GATE><<<grid, 256, 0, st>>>(a, lda, u, ldu, state, state_out, x, B, w);
+        else
+            scan_step<DT, 1, GATE><<<grid, 256, 0, st>>>(a, lda, u, ldu, state, state_out, x, B, w);
         return hipGetLastError();
     });
 }

@@ -171,6 +171,24 @@ def test_zero_rows_and_eps(dev):
     both(v, no.SILU, torch.float32, eps=0.5)
 
 
+def test_beyond_32_bit_offsets(dev):
+    """More than 2^31 elements: the last rows as a call on them alone has them."""
+    n, w = 270000, 8192
+    assert n * w > 1 << 31
+    x = torch.empty((1, n, w), dtype=torch.bfloat16, device=dev).normal_()
+    y = torch.empty_like(x).normal_()
+    pre, post = torch.ones(w, device=dev), torch.ones(w, device=dev)
+    f = deeppcr.deeppcr_residual_norm_forward(x, y, w_post=post, w_pre=pre)
+    tail = lambda t: t[:, -5:].contiguous()
+    g = deeppcr.deeppcr_residual_norm_forward(tail(x), tail(y), w_post=post, w_pre=pre)
+    assert torch.equal(tail(f.x_out), g.x_out) and torch.equal(tail(f.h), g.h)
+    b = deeppcr.deeppcr_residual_norm_backward(x, y, f.rstd_post, f.rstd_pre, dh=x, w_post=post,
+                                               w_pre=pre)
+    c = deeppcr.deeppcr_residual_norm_backward(tail(x), tail(y), g.rstd_post, g.rstd_pre,
+                                               dh=tail(x), w_post=post, w_pre=pre)
+    assert torch.equal(tail(b.dx), c.dx) and torch.equal(tail(b.dy), c.dy)
+
+
 def test_stream_in_place(dev):
     v = inputs(2, 9, 1000, no.SILU, False, torch.bfloat16, dev)
     p = {k: v[k] for k in ("z", "w_post", "scale", "w_pre")}

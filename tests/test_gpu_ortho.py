@@ -29,7 +29,7 @@ torch = pytest.importorskip("torch")
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 SHAPES = [(1, 1, 1), (3, 1, 5), (2, 5, 1), (4, 2, 2), (5, 16, 16), (3, 17, 17), (7, 32, 32),
           (2, 31, 33), (3, 64, 64), (2, 40, 64), (2, 100, 100), (3, 128, 128), (2, 128, 16),
-          (2, 16, 128), (2, 129, 129), (1, 96, 200), (2, 200, 96), (1, 256, 256), (1, 1, 300),
+          (2, 16, 128), (2, 50, 100), (2, 90, 120), (2, 120, 70), (2, 60, 20), (2, 129, 129), (1, 96, 200), (2, 200, 96), (1, 256, 256), (1, 1, 300),
           (1, 333, 130), (1, 520, 264), (1, 130, 1025)]
 
 
@@ -97,6 +97,29 @@ def test_range(dev, w):
     keep = [0, 1, 2, 3, 6, 7]
     assert torch.equal(bad[keep], got[keep])
     assert torch.isnan(bad[4]).any() and torch.isnan(bad[5]).any()
+
+
+@pytest.mark.parametrize("w", [16, 30, 64, 128, 150])
+def test_gradients_below_eps(dev, w):
+    """|G| / eps from 10 down to 1e-20: X is small, and moved by its linear term
+    until it has grown; its own size bounds its error."""
+    scale = 10.0 ** torch.arange(1.0, -21.0, -3.0)
+    G = gradient(len(scale), w, w, torch.float32, dev)
+    G *= (scale * 1e-7).to(dev)[:, None, None] / torch.linalg.matrix_norm(G)[:, None, None]
+    for steps, coeffs in ((5, oo.COEFFS), (12, (1.5, -0.5, 0.0)), (3, (0.5, 0.25, 0.0))):
+        got = deeppcr.deeppcr_orthogonalize(G, steps=steps, coeffs=coeffs)
+        check(got, oo.orthogonalize(cpu(G), steps, coeffs), torch.float32, steps, coeffs)
+
+
+def test_more_matrices_than_a_launch_works_on(dev):
+    """The stack goes through the workspace in parts."""
+    N, m, n = 9000, 3, 130
+    few = deeppcr.orthogonalize_workspace_bytes(100, m, n) / 100
+    assert deeppcr.orthogonalize_workspace_bytes(N, m, n) < few * N
+    G = gradient(N, m, n, torch.float32, dev)
+    got = deeppcr.deeppcr_orthogonalize(G)
+    for part in (slice(0, 4), slice(7000, 7400), slice(N - 4, N)):
+        assert torch.equal(got[part], deeppcr.deeppcr_orthogonalize(G[part].contiguous()))
 
 
 def test_in_place_and_same_bits(dev):

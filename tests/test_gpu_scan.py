@@ -149,6 +149,42 @@ def test_slices_of_a_projection(dev, kind, size):
         both(*t, None, gate, TYPES[kind])
 
 
+def test_many_channels_walk_their_tiles(dev):
+    """More groups of channels than run at once (513 of 64 packs): several tiles
+    one after the other in a workgroup, with and without padding."""
+    for dtype, w in ((torch.bfloat16, 2 * 513 * 64), (torch.float32, 513 * 64)):
+        for lengths in (None, [400]):
+            t = inputs(1, 400, w, so.SIGMOID, dtype, dev)
+            both(*t, lengths, so.SIGMOID, dtype)
+
+
+def test_beyond_32_bit_offsets(dev):
+    """A sequence of more than 2^31 elements: the last rows' states forget what is
+    more than 64 halvings back, the first rows' adjoints what is that far ahead."""
+    L, w = 70000, 32768
+    assert L * w > 1 << 31
+    a = torch.full((1, L, w), 0.5, dtype=torch.bfloat16, device=dev)
+    u = torch.empty_like(a)
+    for i in range(0, L, 10000):
+        u[:, i:i + 10000].normal_()
+    x, last = deeppcr.deeppcr_gated_scan_forward(a, u)
+    r = torch.zeros(1, w, dtype=torch.float64, device=dev)
+    for l in range(L - 80, L):
+        r = 0.5 * r + u[:, l].double()
+        if l >= L - 16:
+            assert torch.all((x[:, l].double() - r).abs() <= 2.0 ** -8 * r.abs() + 2.0 ** -20)
+    assert torch.all((last.double() - r).abs() <= 2.0 ** -20 * (1 + r.abs()))
+    da, du, dx0 = deeppcr.deeppcr_gated_scan_backward(a, None, x, u)
+    r = torch.zeros(1, w, dtype=torch.float64, device=dev)
+    for l in reversed(range(80)):
+        r = 0.5 * r + u[:, l].double()
+        if l < 16:
+            assert torch.all((du[:, l].double() - r).abs() <= 2.0 ** -8 * r.abs() + 2.0 ** -20)
+    assert torch.all((dx0.double() - 0.5 * r).abs() <= 2.0 ** -20 * (1 + r.abs()))
+    want = du[:, L - 1].double() * x[:, L - 2].double()
+    assert torch.all((da[:, L - 1].double() - want).abs() <= 2.0 ** -7 * want.abs() + 2.0 ** -30)
+
+
 def test_no_start_and_no_last_gradient(dev):
     a, u, g, _, _ = inputs(2, 600, 40, so.SIGMOID, torch.bfloat16, dev)
     both(a, u, g, None, None, None, so.SIGMOID, torch.bfloat16)
@@ -205,7 +241,7 @@ def test_states_in_place(dev):
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
-@pytest.mark.parametrize("shape", [(1, 1), (3, 5), (2, 64), (256, 130), (1, 4096), (9, 1001)], ids=str)
+@pytest.mark.parametrize("shape", [(1, 1), (3, 5), (2, 64), (256, 130), (1, 4096), (9, 1001), (64, 4100)], ids=str)
 def test_step(dev, kind, shape):
     """Steps one after the other are the rows of the forward pass."""
     B, w = shape

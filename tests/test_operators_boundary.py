@@ -35,8 +35,11 @@ def _step(a=P[0], lda=40, u=P[1], ldu=40, s=P[2], so=P[3], x=P[4], B=2, w=40, ga
 def test_gated_scan_sizes():
     f = deeppcr.gated_scan_workspace_bytes
     assert f(1, 1, 1) > 0 and f(8, 65536, 1024) > 0
-    for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (-1, 4, 4), (1 << 20, 4, 1 << 11)):
+    for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (-1, 4, 4), (1 << 20, 4, 1 << 11),
+                ((1 << 19) + 1, 4, 1 << 10), (1, (1 << 30) + 1, 4)):
         assert f(*bad) == 0
+    # many channels run through a sequence tile after tile and need no board
+    assert f(256, 4096, 8192) == f(1, 1, 1) < f(1, 4096, 8192)
 
 
 @pytest.mark.parametrize("call,required,arrays", [
