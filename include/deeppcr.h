@@ -532,7 +532,8 @@ int deeppcr_residual_norm_backward(const void* x, const void* y, long long ldy, 
  * them towards one and leaves the singular vectors.  A zero matrix stays
  * zero; a NaN or infinity stays in its matrix.
  *   G [N, m, n], X [N, m, n] of type dtype, contiguous; X may be G
- *   steps >= 0; ca, cb, cc finite, and such that the iterates stay moderate:
+ *   steps >= 0; ca, cb, cc finite, |ca| >= 1/16 (the linear term moves small
+ *         singular values), and such that the iterates stay moderate:
  *         with s <= 1 the largest singular value, s and cb s^2 + cc s^4 have
  *         to stay below 15 in every step for every s that can occur, else
  *         DEEPPCR_EINVAL

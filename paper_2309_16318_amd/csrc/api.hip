@@ -1557,10 +1557,13 @@ bool ortho_ok(int N, int m, int n, int dtype) {
 // Follows the largest singular value that an iterate can have: with s in
 // [0, top], |s (ca + q(s))| and q(s) = cb s^2 + cc s^4 take their largest
 // sizes at the ends or where a derivative vanishes (quadratics in s^2).  A
-// slack of 1/1000 stands for the rounding of the products.
-constexpr double kIterateLimit = 15.0;
+// slack of 1/1000 stands for the rounding of the products.  The linear term has
+// to count: small singular values grow by it alone, and a small X is held to the
+// precision that it needs beside it.
+constexpr double kIterateLimit = 15.0, kLeastLinear = 1.0 / 16.0;
 bool iterates_stay(int steps, double ca, double cb, double cc) {
     if (!std::isfinite(ca) || !std::isfinite(cb) || !std::isfinite(cc)) return false;
+    if (std::fabs(ca) < kLeastLinear) return false;
     double top = 1.0;
     for (int i = 0; i < steps; ++i) {
         top *= 1.001;

@@ -12,10 +12,11 @@
 // symmetric: their tiles on and above the diagonal are computed and written
 // twice.
 //
-// A gradient far below eps makes a small X, which only its linear term moves
-// until it has grown.  It is held as Y = 2^e X with e from the norm that the
-// linear term gives it, so that its parts keep their bits:
-//   Y' = 2^(e'-e) (ca Y + (cb 2^-2e A + cc 2^-4e A A) Y),  A = Y Y^T.
+// A gradient far below eps makes a small X.  It is held as Y = 2^e X with 2^-e a
+// bound of its norm, so that its parts keep their bits:
+//   Y' = 2^(e'-e) (ca Y + (cb 2^-2e A + cc 2^-4e A A) Y),  A = Y Y^T;
+// the bound follows s -> |ca| s + |cb| s^3 + |cc| s^5, which is close where only
+// the linear term counts.
 #include <algorithm>
 #include <type_traits>
 
@@ -170,11 +171,25 @@ __device__ __forceinline__ Start start_of(const float4* parts, int n, float eps)
     return {unit, 1.f / den, log2f(den / norm)};
 }
 
-// e of step `step`, for a linear term that multiplies by 2^rate.
-__device__ __forceinline__ int shift_of(float depth, float rate, int step) {
-    const float e = floorf(depth - rate * (float)step);
-    return e > 0.f ? (int)fminf(e, 120.f) : 0;  // 0 where depth is NaN
+// The polynomial's coefficients' sizes; the bound's logarithm after a step (no
+// iterate passes 15); and the shift that goes with it.
+struct Growth {
+    float a, b, c;
+};
+__device__ __forceinline__ float grown(float bound, const Growth& g) {
+    const float s = exp2f(2.f * bound);
+    return fminf(bound + log2f(fmaf(s, fmaf(s, g.c, g.b), g.a)), 4.f);
 }
+__device__ __forceinline__ int shift_of(float bound) {
+    const float e = floorf(-bound);
+    return e > 0.f ? (int)fminf(e, 120.f) : 0;  // 0 where the bound is NaN
+}
+// Of one matrix between the launches: the bound behind the step under way, its
+// shift and the next step's.
+struct Shift {
+    float bound;
+    int now, next;
+};
 
 // The parts of a stack of matrices [rows, cols], padded to whole tiles with
 // zeros, in panels of 32 columns: a row of a panel is 32 hi and 32 lo, one cache
@@ -193,13 +208,14 @@ constexpr int kLo = 32;  // from hi to lo
 // X [kp, rp] from G [m, n] (its transpose where m > n), 64 x 64 at a time.
 template <int DT>
 __global__ void __launch_bounds__(256) ortho_start(const void* G, Panels X, const float4* parts,
-                                                   int nparts, float* depth, int m, int n,
+                                                   int nparts, Shift* shifts, int m, int n,
                                                    float eps) {
     __shared__ float t[64][65];
     const long long z = blockIdx.z;
     const Start s = start_of(parts + z * nparts, nparts, eps);
-    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) depth[z] = s.depth;
-    const float inv = ldexpf(s.inv, shift_of(s.depth, 0.f, 0));
+    const int shift = shift_of(-s.depth);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) shifts[z] = {-s.depth, 0, shift};
+    const float inv = ldexpf(s.inv, shift);
     const bool tall = m > n;
     // rows i0.. and columns j0.. of G, padded like it
     const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
@@ -247,9 +263,8 @@ struct Product {
     void* out;     // last APPLY: X [m, n] instead
     int rows, cols, K;  // padded
     int m, n;
-    const float* depth;
-    float rate;
-    int step;
+    Shift* shifts;
+    Growth growth;
     float own, times;   // own D + times P Q, before the shifts
 };
 
@@ -369,15 +384,25 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
     // values times kScale, as their parts are
     float own = g.own, f = g.times * kUnscale;
     int fin = 0;
-    if constexpr (MODE != GRAM) {
-        const int e = shift_of(g.depth[z], g.rate, g.step);
+    if constexpr (MODE == GRAM) {
+        // the step's first launch moves the shifts on; the others read them
+        if (id % tiles == 0 && threadIdx.x == 0) {
+            Shift s = g.shifts[z];
+            s.bound = grown(s.bound, g.growth);
+            s.now = s.next;
+            s.next = shift_of(s.bound);
+            g.shifts[z] = s;
+        }
+    } else {
+        const Shift s = g.shifts[z];
+        const int e = s.now;
         if constexpr (MODE == POLY) {
             own = ldexpf(own, -2 * e);
             f = ldexpf(f, -4 * e);
         } else if constexpr (OUT >= 0) {
             fin = -e;  // out of the shift; not in the factors, where it may be subnormal
         } else {
-            const int d = shift_of(g.depth[z], g.rate, g.step + 1) - e;
+            const int d = s.next - e;
             own = ldexpf(own, d);
             f = ldexpf(f, d);
         }
@@ -460,12 +485,12 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
 // 1 / (|G| + eps), shifted for the first step, for a matrix whose elements have
 // been divided by the largest, `top`, and then have the square sum `sum`; a zero
 // matrix stays zero, whatever eps, and NaN stays NaN.
-__device__ __forceinline__ float inverse_norm(float top, float sum, float eps, float* depth) {
-    *depth = 0.f;
+__device__ __forceinline__ float inverse_norm(float top, float sum, float eps, float* bound) {
+    *bound = 0.f;
     if (!(top > 0.f)) return sum == sum ? 0.f : sum;
     const float norm = sqrtf(sum), den = norm + eps / top;
-    *depth = log2f(den / norm);
-    return ldexpf(1.f / den, shift_of(*depth, 0.f, 0));
+    *bound = -log2f(den / norm);
+    return ldexpf(1.f / den, shift_of(*bound));
 }
 
 // A matrix of up to 16 x 16 in one wave's registers: element e of a lane is row
@@ -477,7 +502,7 @@ __device__ __forceinline__ float inverse_norm(float top, float sum, float eps, f
 template <int DT>
 __global__ void __launch_bounds__(64) ortho_tiny(const void* G, void* out, int m, int n, int steps,
                                                  float ca, float cb, float cc, float eps,
-                                                 float rate) {
+                                                 Growth growth) {
     typedef float f32x4 __attribute__((ext_vector_type(4)));
     constexpr int NP = 3;
     const int lane = threadIdx.x, col = lane & 15, row0 = lane >> 4 << 2;
@@ -504,8 +529,9 @@ __global__ void __launch_bounds__(64) ortho_tiny(const void* G, void* out, int m
             sum = fmaf(v[e], v[e], sum);
         }
     for (int s = 1; s < 64; s *= 2) sum += __shfl_xor(sum, s);
-    float depth;
-    const float inv = inverse_norm(top, sum + bad, eps, &depth);
+    float bound;
+    const float inv = inverse_norm(top, sum + bad, eps, &bound);
+    int e = shift_of(bound);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] *= inv * kScale;
     h16x4 x[NP];
@@ -535,7 +561,8 @@ __global__ void __launch_bounds__(64) ortho_tiny(const void* G, void* out, int m
     };
     const float f = kUnscale;
     for (int s = 0; s < steps; ++s) {
-        const int e = shift_of(depth, rate, s);
+        bound = grown(bound, growth);
+        const int next = shift_of(bound);
         h16x4 y[NP];
 #pragma unroll
         for (int p = 0; p < NP; ++p) y[p] = turned(x[p]);
@@ -544,7 +571,7 @@ __global__ void __launch_bounds__(64) ortho_tiny(const void* G, void* out, int m
         const f32x4 B = A * ldexpf(cb, -2 * e) + product(y, y) * ldexpf(cc * f, -4 * e);
         parts(B, y);
         const bool last = s + 1 == steps;
-        const int d = last ? 0 : shift_of(depth, rate, s + 1) - e;
+        const int d = last ? 0 : next - e;
         f32x4 c = product(y, x) * ldexpf(f, d);
         const float own = ldexpf(ca, d);
 #pragma unroll
@@ -554,10 +581,11 @@ __global__ void __launch_bounds__(64) ortho_tiny(const void* G, void* out, int m
             v[i] = last ? ldexpf(c[i], -e) : c[i];
         }
         split(v, x);
+        e = next;
     }
     if (steps == 0)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = ldexpf(v[i], -shift_of(depth, 0.f, 0));
+        for (int i = 0; i < 4; ++i) v[i] = ldexpf(v[i], -e);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float one[1] = {v[i] * kUnscale};
@@ -572,7 +600,7 @@ __global__ void __launch_bounds__(64) ortho_tiny(const void* G, void* out, int m
 template <int P, int RT, int DT>
 __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out, int m, int n,
                                                         int steps, float ca, float cb, float cc,
-                                                        float eps, float rate) {
+                                                        float eps, Growth growth) {
     constexpr int NT = P / 32, PITCH = P + 8;  // a row's 16 bytes more spread the banks
     // Sums of few products have no rounding of their own to hide two parts' in
     // (4 x 4 matrices erred by 1.5 times what float32 products do, 11 x 11 by up
@@ -627,8 +655,9 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
     __syncthreads();
     sum = bad;
     for (int v = 0; v < NT; ++v) sum += red[0][v];
-    float depth;
-    const float inv = inverse_norm(top, sum, eps, &depth);
+    float bound;
+    const float inv = inverse_norm(top, sum, eps, &bound);
+    int e = shift_of(bound);
     h16x8 x[RT][2][NP];
     // X's parts from four values times kScale
     auto keep = [&](int t, int q, const float (&v)[4]) {
@@ -704,7 +733,7 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
     // One tile, one wave: A and B are symmetric, so that a lane's column, as a
     // product leaves it, is its row as the left operand too: they never leave the
     // registers.  X crosses LDS for the Gram product.
-    auto one_tile = [&](int s, int e) {
+    auto one_tile = [&](bool last, int e, int next) {
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -746,8 +775,7 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
                     for (int i = 0; i < 4; ++i) to[q / 2][p][4 * (q & 1) + i] = part[p][i];
             }
         };
-        const bool last = s + 1 == steps;
-        const int d = last ? 0 : shift_of(depth, rate, s + 1) - e;
+        const int d = last ? 0 : next - e;
         h16x8 y[2][NP];
         const f32x16 A = times_of(rows, rows) * f;
         parts_of(A, y);
@@ -766,10 +794,14 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
         else
             parts_of(v, x[0]);
     };
+    int next = e;
     for (int s = 0; s < steps; ++s) {
-        const int e = shift_of(depth, rate, s);
+        e = next;
+        bound = grown(bound, growth);
+        next = shift_of(bound);
+        const bool last = s + 1 == steps;
         if constexpr (NT == 1) {
-            one_tile(s, e);
+            one_tile(last, e, next);
             continue;
         }
         const bool square = wave < RT;
@@ -842,8 +874,7 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
 #pragma unroll
                     for (int p = 0; p < NP; ++p) b[p] = x[c / 2][c % 2][p];
                 });
-        const bool last = s + 1 == steps;
-        const int d = last ? 0 : shift_of(depth, rate, s + 1) - e;
+        const int d = last ? 0 : next - e;
         const float own = ldexpf(ca, d), times = ldexpf(f, d);
 #pragma unroll
         for (int t = 0; t < RT; ++t)
@@ -865,7 +896,6 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
             }
     }
     if (steps == 0) {
-        const int e = shift_of(depth, 0.f, 0);
 #pragma unroll
         for (int t = 0; t < RT; ++t)
 #pragma unroll
@@ -925,7 +955,7 @@ template <int DT>
 hipError_t run_small(const void* G, void* X, int N, int m, int n, int steps, float ca, float cb,
                      float cc, float eps, hipStream_t st) {
     const int side = std::max(m, n);
-    const float rate = ca == 0.f ? 0.f : log2f(fabsf(ca));
+    const Growth growth{fabsf(ca), fabsf(cb), fabsf(cc)};
     const long long sz = (long long)m * n * sizeof(elem_t<DT>);
     // a launch has fewer than 2^32 threads
     for (long long at = 0; at < N; at += 1 << 23) {
@@ -934,7 +964,7 @@ hipError_t run_small(const void* G, void* X, int N, int m, int n, int steps, flo
         void* x = (char*)X + at * sz;
         auto go = [&](auto p, auto rt) {
             constexpr int P = decltype(p)::value, RT = decltype(rt)::value;
-            ortho_small<P, RT, DT><<<some, 2 * P, 0, st>>>(g, x, m, n, steps, ca, cb, cc, eps, rate);
+            ortho_small<P, RT, DT><<<some, 2 * P, 0, st>>>(g, x, m, n, steps, ca, cb, cc, eps, growth);
         };
         constexpr std::integral_constant<int, 1> one{};
         constexpr std::integral_constant<int, 2> two{};
@@ -942,7 +972,7 @@ hipError_t run_small(const void* G, void* X, int N, int m, int n, int steps, flo
         constexpr std::integral_constant<int, 4> four{};
         const int rt = (std::min(m, n) + 31) / 32;
         if (side <= 16) {
-            ortho_tiny<DT><<<some, 64, 0, st>>>(g, x, m, n, steps, ca, cb, cc, eps, rate);
+            ortho_tiny<DT><<<some, 64, 0, st>>>(g, x, m, n, steps, ca, cb, cc, eps, growth);
         } else if (side <= 32) {
             go(std::integral_constant<int, 32>{}, one);
         } else if (side <= 64) {
@@ -964,14 +994,13 @@ hipError_t run(const void* G, void* X, int N, int m, int n, int steps, float ca,
     if (small_side(m, n)) return run_small<DT>(G, X, N, m, n, steps, ca, cb, cc, eps, st);
     const Plan p = plan_of(N, m, n);
     const long long sz = (long long)m * n;
-    // a linear term that vanishes leaves nothing to hold on to
-    const float rate = ca == 0.f ? 0.f : log2f(fabsf(ca));
+    const Growth growth{fabsf(ca), fabsf(cb), fabsf(cc)};
     for (long long at = 0; at < N; at += p.some) {
         const int some = (int)std::min<long long>(p.some, N - at);
         const void* g = (const char*)G + at * sz * sizeof(elem_t<DT>);
         void* out = (char*)X + at * sz * sizeof(elem_t<DT>);
         float4* parts = (float4*)ws;
-        float* depth = (float*)(parts + p.some * kParts);
+        Shift* shifts = (Shift*)(parts + p.some * kParts);
         char* q = ws + (size_t)p.some * (kParts + 16) * sizeof(float4);
         // X, A and B take turns in three buffers of X's size
         const long long xn = (long long)p.kp * p.rp, an = (long long)p.kp * p.kp;
@@ -989,17 +1018,17 @@ hipError_t run(const void* G, void* X, int N, int m, int n, int steps, float ca,
         }
         const int gr = m > n ? p.rp : p.kp, gc = m > n ? p.kp : p.rp;
         ortho_start<DT><<<dim3(gc / 64, gr / 64, some), 256, 0, st>>>(
-            g, Panels{buf[0], xn, p.kp}, parts, p.parts, depth, m, n, eps);
+            g, Panels{buf[0], xn, p.kp}, parts, p.parts, shifts, m, n, eps);
         e = hipGetLastError();
         for (int s = 0; s < steps && e == hipSuccess; ++s) {
             const Panels x{buf[0], xn, p.kp}, A{buf[1], an, p.kp}, B{buf[2], an, p.kp},
                 y{buf[1], xn, p.kp};  // over A
-            e = product<GRAM, -1>({x, x, A, nullptr, p.kp, p.kp, p.rp, m, n, depth, rate, s, 0.f, 1.f},
+            e = product<GRAM, -1>({x, x, A, nullptr, p.kp, p.kp, p.rp, m, n, shifts, growth, 0.f, 1.f},
                                   some, st);
             if (e == hipSuccess)
-                e = product<POLY, -1>({A, A, B, nullptr, p.kp, p.kp, p.kp, m, n, depth, rate, s, cb, cc},
+                e = product<POLY, -1>({A, A, B, nullptr, p.kp, p.kp, p.kp, m, n, shifts, growth, cb, cc},
                                       some, st);
-            const Product last{B, x, y, out, p.kp, p.rp, p.kp, m, n, depth, rate, s, ca, 1.f};
+            const Product last{B, x, y, out, p.kp, p.rp, p.kp, m, n, shifts, growth, ca, 1.f};
             if (e == hipSuccess)
                 e = s + 1 < steps ? product<APPLY, -1>(last, some, st)
                                   : product<APPLY, DT>(last, some, st);

@@ -66,13 +66,17 @@ __device__ __forceinline__ unsigned long long peek(const unsigned long long* p) 
 }
 // Waits for a word of a tile with a smaller ticket, given as it was at first:
 // that tile's workgroup is running, and what it still waits for has a smaller
-// ticket again.
+// ticket again.  A board that another call writes to at the same time (which the
+// interface forbids) may never have the word: the wait ends after kPatience
+// looks, some ten seconds, with NaN.
+constexpr int kPatience = 1 << 24;
 __device__ __forceinline__ void await(const unsigned long long* p, unsigned long long v, float* A,
                                       float* H) {
-    while (v == kEmpty) {
+    for (int i = 0; v == kEmpty && i < kPatience; ++i) {
         __builtin_amdgcn_s_sleep(1);
         v = peek(p);
     }
+    // kEmpty itself is a pair of NaN
     *A = __uint_as_float((unsigned)v);
     *H = __uint_as_float((unsigned)(v >> 32));
 }
@@ -122,6 +126,7 @@ __global__ void __launch_bounds__(64 * S, 4) scan_tile(ScanArgs k, Board bd, int
         if (threadIdx.x == 0) ticket = atomicAdd(bd.tickets + grp * kApart, 1u);
         __syncthreads();
         c0 = __builtin_amdgcn_readfirstlane(ticket);
+        if (c0 >= chunks) return;  // only on a board that another call cleared meanwhile
     }
     const int c1 = SPLIT ? c0 + 1 : chunks;
     // pack f of all sequences' channels: sequence b, channels c .. c+V-1

@@ -189,6 +189,11 @@ def test_beyond_32_bit_offsets(dev):
     assert torch.equal(tail(b.dx), c.dx) and torch.equal(tail(b.dy), c.dy)
 
 
+def test_more_sequences_than_a_grids_axis(dev):
+    """One gate for each of 33000 sequences."""
+    both(inputs(33000, 2, 8, no.SILU, True, torch.float32, dev), no.SILU, torch.float32)
+
+
 def test_stream_in_place(dev):
     v = inputs(2, 9, 1000, no.SILU, False, torch.bfloat16, dev)
     p = {k: v[k] for k in ("z", "w_post", "scale", "w_pre")}

@@ -111,6 +111,28 @@ def test_gradients_below_eps(dev, w):
         check(got, oo.orthogonalize(cpu(G), steps, coeffs), torch.float32, steps, coeffs)
 
 
+@pytest.mark.parametrize("w", [16, 30, 64, 150])
+def test_a_linear_term_that_counts_least(dev, w):
+    """Iterates that the cubic term makes, far larger than the linear term alone
+    would have them.  They are held to the bound u -> |a| u + |b| u^3 + |c| u^5 of
+    their norms, here far above them: a step adds an error of 2^-20 u' (its
+    operands' 22 bits, against their bounds), and later steps magnify it by at most
+    their slope |a| + 3 |b| u^2 + 5 |c| u^4 <= 5 u' / u, so that three steps end
+    within (25 + 5 + 1) 2^-20 of the last bound."""
+    G = gradient(3, w, w, torch.float32, dev)
+    G[1] *= 1e-7 / torch.linalg.matrix_norm(G[1])          # X = 1 / 2
+    G[2] = torch.outer(G[2, 0], G[2, 1]) * 1e-6            # one singular value, small
+    for coeffs in ((0.0625, 0.9375, 0.0), (0.0625, 1.0, -0.1), (-0.0625, 0.0, 1.0)):
+        got = cpu(deeppcr.deeppcr_orthogonalize(G, steps=3, coeffs=coeffs))
+        ref = oo.orthogonalize(cpu(G), 3, coeffs)
+        norm = np.linalg.norm(cpu(G), axis=(1, 2))
+        u = norm / (norm + 1e-7)
+        for _ in range(3):
+            u = abs(coeffs[0]) * u + abs(coeffs[1]) * u ** 3 + abs(coeffs[2]) * u ** 5
+        err = np.max(np.abs(got - ref), axis=(1, 2))
+        assert np.all(np.isfinite(got)) and np.all(err <= 31 * 2.0 ** -20 * u), (coeffs, err / u)
+
+
 def test_more_matrices_than_a_launch_works_on(dev):
     """The stack goes through the workspace in parts."""
     N, m, n = 9000, 3, 130

@@ -179,10 +179,10 @@ def test_orthogonalize_rejects_invalid_arguments():
 def test_orthogonalize_rejects_polynomials_that_run_away():
     W = deeppcr.EWORKSPACE        # a valid call with a short workspace
     assert _ortho(nws=1) == W
-    for ok in ((1.5, -0.5, 0.0), (1.875, -1.25, 0.375), (3.4445, -4.7750, 2.0315), (0, 0, 0),
-               (1, 0, 0)):
+    for ok in ((1.5, -0.5, 0.0), (1.875, -1.25, 0.375), (3.4445, -4.7750, 2.0315),
+               (0.0625, 0, 0), (-1, 0, 0), (1, 0, 0)):
         assert _ortho(a=ok[0], b=ok[1], c=ok[2], steps=8, nws=1) == W, ok
-    for bad in ((100.0, 0, 0), (3.4445, 4.7750, 2.0315), (2.0, 0, 0), (1.5, -0.5, 30.0),
+    for bad in ((0, 0, 0), (0.06, 1, 0), (100.0, 0, 0), (3.4445, 4.7750, 2.0315), (2.0, 0, 0), (1.5, -0.5, 30.0),
                 (float("nan"), 0, 0), (1, float("inf"), 0)):
         assert _ortho(a=bad[0], b=bad[1], c=bad[2], steps=8, nws=1) == E, bad
     assert _ortho(a=2.0, b=0, c=0, steps=2, nws=1) == W
