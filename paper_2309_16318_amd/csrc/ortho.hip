@@ -192,18 +192,18 @@ struct Shift {
 };
 
 // The parts of a stack of matrices [rows, cols], padded to whole tiles with
-// zeros, in panels of 32 columns: a row of a panel is 32 hi and 32 lo, one cache
-// line, and the rows of a panel follow each other, so that a tile's share of a
-// step is one run of memory.
+// zeros, in panels of 16 columns: a row of a panel is 16 hi and 16 lo, and the
+// rows of a panel follow each other, so that a tile's share of a step is one run
+// of memory.
 struct Panels {
     h16* p;
     long long sz;  // rows * cols
     int rows;
     __device__ __forceinline__ h16* at(long long z, int row, int col) const {
-        return p + 2 * z * sz + ((long long)(col >> 5) * rows + row) * 64 + (col & 31);
+        return p + 2 * z * sz + ((long long)(col >> 4) * rows + row) * 32 + (col & 15);
     }
 };
-constexpr int kLo = 32;  // from hi to lo
+constexpr int kLo = 16;  // from hi to lo
 
 // X [kp, rp] from G [m, n] (its transpose where m > n), 64 x 64 at a time.
 template <int DT>
@@ -269,13 +269,17 @@ struct Product {
 };
 
 // One tile of BM x BM per workgroup of 2 x 2 waves, in turn over the matrices
-// so that an XCD (workgroups go to the 8 of them in turn) works on few.
+// so that an XCD (workgroups go to the 8 of them in turn) works on few.  Steps of
+// 16 columns leave room for four workgroups on a CU, which hide each other's
+// loads and barriers: 16 matrices of 1024 x 1024 1.35 ms a call, against 1.49 with
+// two workgroups, steps of 32 and the loads two steps ahead in registers.
 template <int BM, int MODE, int OUT>
-__global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, long long all) {
-    constexpr int BK = 32, MT = BM / 64;
-    constexpr int LD = BM * 8 / 256;          // 16-byte chunks of an operand per thread
+__global__ void __launch_bounds__(256, 4) ortho_product(Product g, int tiles, long long all) {
+    constexpr int BK = 16, MT = BM / 64;
+    constexpr int LD = BM / 64;  // loads of 64 chunks of an operand per wave
     __shared__ __attribute__((aligned(16))) h16 sm[2][2][BM * 2 * BK];  // buffer, operand
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long long per = (all + 7) / 8, id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= per || id >= all) return;
     const long long z = id / tiles;
@@ -293,92 +297,78 @@ __global__ void __launch_bounds__(256, 2) ortho_product(Product g, int tiles, lo
         bi = t - bj * (bj + 1) / 2;
     }
     // An operand's tile in a step: BM rows of one panel, or (APPLY's right one)
-    // 32 rows of BM / 32 panels, whose columns are read across.
+    // 16 rows of BM / 16 panels, whose columns are read across.
     constexpr bool ACROSS = MODE == APPLY;
     const h16* src[2] = {g.P.at(z, bi * BM, 0),
                          ACROSS ? g.Q.at(z, 0, bj * BM) : g.Q.at(z, bj * BM, 0)};
-    const long long ahead[2] = {g.P.rows * 64LL, ACROSS ? 32 * 64LL : g.Q.rows * 64LL};
-    // Two steps' loads are on their way while one is worked on: a step's
-    // products take 0.6 us, a load under load longer.
-    h16x8 st[2][2][LD];
-    auto fetch = [&](h16x8 (&to)[2][LD], int s) {
-#pragma unroll
-        for (int o = 0; o < 2; ++o)
-#pragma unroll
-            for (int u = 0; u < LD; ++u) {
-                const int q = threadIdx.x + 256 * u;
-                const long long at = ACROSS && o == 1 ? (q >> 8) * (g.Q.rows * 64LL) + (q & 255) * 8
-                                                      : q * 8;
-                to[o][u] = *reinterpret_cast<const h16x8*>(src[o] + s * ahead[o] + at);
-            }
-    };
-    // chunk c of a row (4 of hi, 4 of lo) sits at c ^ (row / 2 mod 8): 16 rows
+    const long long ahead[2] = {g.P.rows * 32LL, ACROSS ? 16 * 32LL : g.Q.rows * 32LL};
+    // chunk c of a row (2 of hi, 2 of lo) sits at c ^ (row / 4 mod 4): 16 rows
     // that are read together lie in different banks
-    auto chunk = [](int row, int c) { return row * 64 + (c ^ ((row >> 1) & 7)) * 8; };
-    auto place = [&](const h16x8 (&from)[2][LD], int b) {
+    auto chunk = [](int row, int c) { return row * 32 + (c ^ ((row >> 2) & 3)) * 8; };
+    // A step's tiles go from memory to LDS without passing registers: a wave's
+    // load fills 64 chunks in the lanes' order, so each lane asks for the chunk
+    // that belongs there.
+    typedef const __attribute__((address_space(1))) void* Global;
+    typedef __attribute__((address_space(3))) void* Lds;
+    long long from[2][LD];
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+#pragma unroll
+        for (int u = 0; u < LD; ++u) {
+            const int row = (u * 4 + wave) * 16 + (lane >> 2), c = (lane & 3) ^ ((row >> 2) & 3);
+            from[o][u] = ACROSS && o == 1 ? (row >> 4) * (g.Q.rows * 32LL) + (row & 15) * 32 + c * 8
+                                          : row * 32 + c * 8;
+        }
+    auto stage = [&](int buf, int s) {
 #pragma unroll
         for (int o = 0; o < 2; ++o)
 #pragma unroll
-            for (int u = 0; u < LD; ++u) {
-                const int q = threadIdx.x + 256 * u;
-                *reinterpret_cast<h16x8*>(&sm[b][o][chunk(q >> 3, q & 7)]) = from[o][u];
-            }
+            for (int u = 0; u < LD; ++u)
+                __builtin_amdgcn_global_load_lds((Global)(src[o] + s * ahead[o] + from[o][u]),
+                                                 (Lds)&sm[buf][o][(u * 4 + wave) * 512], 16, 0, 0);
     };
     const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BM / 2);
     const int r32 = lane & 31, half = lane >> 5;
     f32x16 acc[MT][MT] = {};
     const int steps = g.K / BK;
-    auto multiply = [&](int buf) {
+    stage(0, 0);
+    for (int s = 0; s < steps; ++s) {
+        // this step's tiles have arrived, and nobody reads the other buffer any more
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        const int buf = s & 1;
+        h16x8 a[MT][2], b[MT][2];
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            h16x8 a[MT][2], b[MT][2];
+        for (int t = 0; t < MT; ++t)
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
+            for (int p = 0; p < 2; ++p) {
+                a[t][p] = *reinterpret_cast<const h16x8*>(&sm[buf][0][chunk(wm + t * 32 + r32, p * 2 + half)]);
+                if constexpr (ACROSS) {
+                    // lane 4 i + j of 16 gives row i, columns 4 j .. 4 j + 3 of a 4 x 16
+                    // block and gets its column 4 i + j
+                    h16x4 v[2];
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    const int c = p * 4 + kk * 2 + half;
-                    a[t][p] = *reinterpret_cast<const h16x8*>(&sm[buf][0][chunk(wm + t * 32 + r32, c)]);
-                    if constexpr (ACROSS) {
-                        // lane 4 i + j of 16 gives row i, columns 4 j .. 4 j + 3 of a 4 x 16
-                        // block and gets its column 4 i + j
-                        h16x4 v[2];
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            const int k = wn + t * 32 + kk * 16 + half * 8 + u * 4 + ((lane & 15) >> 2);
-                            const int x = (lane & 16) + (lane & 3) * 4;
-                            v[u] = read_across(&sm[buf][1][chunk(k, p * 4 + (x >> 3)) + (x & 7)]);
-                        }
-                        b[t][p] = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
-                    } else {
-                        b[t][p] = *reinterpret_cast<const h16x8*>(
-                            &sm[buf][1][chunk(wn + t * 32 + r32, c)]);
+                    for (int u = 0; u < 2; ++u) {
+                        const int k = wn + t * 32 + (lane & 16) + half * 8 + u * 4 + ((lane & 15) >> 2);
+                        v[u] = read_across(&sm[buf][1][chunk(k, p * 2 + ((lane & 3) >> 1)) + (lane & 1) * 4]);
                     }
+                    b[t][p] = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                } else {
+                    b[t][p] = *reinterpret_cast<const h16x8*>(&sm[buf][1][chunk(wn + t * 32 + r32, p * 2 + half)]);
                 }
+            }
+        // (the compiler would wait for these loads before any later read of LDS)
+        __builtin_amdgcn_sched_barrier(0);
+        if (s + 1 < steps) stage(buf ^ 1, s + 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int p = 0; p < 3; ++p)
+        for (int p = 0; p < 3; ++p)
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+            for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int j = 0; j < MT; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                            a[i][p == 0], b[j][p == 1], acc[i][j], 0, 0, 0);
-        }
-    };
-    // step s from buffer s & 1; the step after it waits in st[(s + 1) & 1]
-    fetch(st[0], 0);
-    if (steps > 1) fetch(st[1], 1);
-    place(st[0], 0);
-    __syncthreads();
-    for (int s = 0; s < steps; s += 2) {
-        if (s + 2 < steps) fetch(st[0], s + 2);
-        multiply(0);
-        if (s + 1 < steps) place(st[1], 1);
-        __syncthreads();
-        if (s + 1 >= steps) break;
-        if (s + 3 < steps) fetch(st[1], s + 3);
-        multiply(1);
-        if (s + 2 < steps) place(st[0], 0);
-        __syncthreads();
+                for (int j = 0; j < MT; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][p == 0], b[j][p == 1],
+                                                                       acc[i][j], 0, 0, 0);
     }
     // a lane holds column r32 of each 32 x 32 tile, rows 8 q + 4 half + 0 .. 3
     // values times kScale, as their parts are
