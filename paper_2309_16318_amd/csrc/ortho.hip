@@ -902,9 +902,10 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
 }
 
 // ------------------------------------------------------------------- the plan
-// Sides are padded to whole tiles: 128 from 512 on (at most a quarter more),
-// 64 below.
-int padded(int n) { return n >= 512 ? (n + 127) / 128 * 128 : (n + 63) / 64 * 64; }
+// Sides are padded to whole tiles of 64.  (To tiles of 128, from 512 on or above
+// 64: five of 960 x 960 597 us, 26 of 448 x 448 383, 192 of 140 x 140 492, against
+// 476, 291 and 310.)
+int padded(int n) { return (n + 63) / 64 * 64; }
 
 struct Plan {
     int k, r, kp, rp, parts;
@@ -926,9 +927,15 @@ Plan plan_of(int N, int m, int n) {
 
 template <int MODE, int OUT>
 hipError_t product(const Product& g, int some, hipStream_t st) {
-    const int BM = g.rows % 128 == 0 && g.cols % 128 == 0 ? 128 : 64;
-    const long long ti = g.rows / BM, tj = g.cols / BM;
-    const int tiles = (int)(MODE == APPLY ? ti * tj : ti * (ti + 1) / 2);
+    // Tiles of 128, which read LDS and L2 half as much, where there is more than
+    // one for every CU: 8 of 1024 x 1024 694 us against 767 with tiles of 64, 16
+    // 1349 and 1436, 64 of 512 x 512 805 and 861, but 4 of 1024 x 1024 585 and 490.
+    auto tiles_of = [&](int side) {
+        const long long ti = g.rows / side, tj = g.cols / side;
+        return (int)(MODE == APPLY ? ti * tj : ti * (ti + 1) / 2);
+    };
+    const bool large = g.rows % 128 == 0 && g.cols % 128 == 0 && tiles_of(128) * (long long)some > 256;
+    const int BM = large ? 128 : 64, tiles = tiles_of(BM);
     const long long all = tiles * (long long)some;
     const unsigned grid = (unsigned)((all + 7) / 8 * 8);
     if (BM == 128)

@@ -30,7 +30,9 @@ TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 SHAPES = [(1, 1, 1), (3, 1, 5), (2, 5, 1), (4, 2, 2), (5, 16, 16), (3, 17, 17), (7, 32, 32),
           (2, 31, 33), (3, 64, 64), (2, 40, 64), (2, 100, 100), (3, 128, 128), (2, 128, 16),
           (2, 16, 128), (2, 50, 100), (2, 90, 120), (2, 120, 70), (2, 60, 20), (2, 129, 129), (1, 96, 200), (2, 200, 96), (1, 256, 256), (1, 1, 300),
-          (1, 333, 130), (1, 520, 264), (1, 130, 1025)]
+          (1, 333, 130), (1, 520, 264), (1, 130, 1025),
+          # more large tiles than CUs
+          (270, 128, 250), (260, 250, 120), (90, 250, 256)]
 
 
 @pytest.fixture(scope="module")
