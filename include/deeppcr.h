@@ -423,7 +423,8 @@ enum {
  *   x_last  [B, w] float32, output, or NULL: the state after row
  *           lengths[b] - 1 (x0 for an empty sequence), not rounded to dtype;
  *           may be x0
- * The state is float32 throughout; x is its rounding.  Long sequences are cut
+ * The state is float32 throughout; x is its rounding.  A sigmoid below 2^-126
+ * counts as zero.  Long sequences are cut
  * into chunks of rows that are solved at once from the products of their
  * multipliers, so a direct gate's products over consecutive rows have to stay
  * inside the float32 range (those of multipliers in [-1, 1] do; an underflow
@@ -479,7 +480,8 @@ int deeppcr_gated_scan_step(const void* a, long long lda, const void* u, long lo
  *   yn = w_post * y * rstd_post,          rstd_post = 1 / sqrt(mean(y^2) + eps)
  *   x_out = x + scale * act(z) * yn
  *   h = w_pre * x_out * rstd_pre,         rstd_pre = 1 / sqrt(mean(x_out^2) + eps)
- * each over the w channels; h is formed from x_out before its rounding.
+ * each over the w channels; h is formed from x_out before its rounding.  A
+ * row's squares have to stay in the float32 range.
  *   x [B, L, w] the stream;  y [B, L, w] the block's output, row stride ldy,
  *         or NULL: there is none, and h is the norm of x (the front of a
  *         stack; z, w_post, scale, x_out have to be NULL, gate NONE)
@@ -567,6 +569,7 @@ enum {
     DEEPPCR_KCLASS_OTHER = 4,      /* initial guess, copies, dz0               */
     DEEPPCR_KCLASS_SEQUENTIAL = 5, /* sequential baseline passes               */
     DEEPPCR_KCLASS_PCR_TAIL = 6,   /* substitution inside chunks, or row by row */
+    /* one count per call: */
     DEEPPCR_KCLASS_SCAN = 7,       /* gated scan                               */
     DEEPPCR_KCLASS_NORM = 8,       /* residual norm                            */
     DEEPPCR_KCLASS_ORTHO = 9,      /* orthogonalised update                    */

@@ -81,10 +81,20 @@ struct Raw {
     }
 };
 
-// s = sigmoid(a) and c = 1 - s, each to full relative precision: with
-// t = exp(-|a|) in (0, 1] neither overflows nor cancels.  NaN gives NaN.
+// s = sigmoid(a) and c = 1 - s: with t = exp(-|a|) in (0, 1] neither overflows
+// nor cancels.  NaN gives NaN, a t below 2^-126 zero.  The exponential of the
+// rounded product with log2(e) is off by |a| 2^-24; FINE, for float32 results,
+// makes that up from the product's rest (four instructions more).
+template <bool FINE>
 __device__ __forceinline__ void sigmoid_pair(float a, float* s, float* c) {
-    const float t = __expf(-fabsf(a));
+    constexpr float kLog2e = 0x1.715476p+0f, kRest = 0x1.4ae0c00000000p-26f, kLn2 = 0x1.62e43p-1f;
+    const float x = -fabsf(a), h = x * kLog2e;
+    float t = __builtin_amdgcn_exp2f(h);
+    if constexpr (FINE) {
+        const float r = fmaf(x, kRest, fmaf(x, kLog2e, -h));
+        // (an infinite a has no rest, and a zero t needs none)
+        t = t > 0.f ? fmaf(t, r * kLn2, t) : t;
+    }
     const float big = __builtin_amdgcn_rcpf(1.f + t), small = t * big;
     *s = a >= 0.f ? big : small;
     *c = a >= 0.f ? small : big;

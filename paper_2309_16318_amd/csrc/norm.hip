@@ -140,6 +140,7 @@ struct RowSum {
 };
 
 // The gate's value, and its slope where `slope` is given.
+template <int DT>
 __device__ __forceinline__ void gate_values(int gate, const float (&z)[E], float (&v)[E],
                                             float* slope) {
     if (gate == 0 || gate == 3) {
@@ -153,7 +154,7 @@ __device__ __forceinline__ void gate_values(int gate, const float (&z)[E], float
 #pragma unroll
     for (int j = 0; j < E; ++j) {
         float s, c;
-        sigmoid_pair(z[j], &s, &c);
+        sigmoid_pair<DT == 0>(z[j], &s, &c);
         v[j] = gate == 1 ? s : z[j] * s;
         if (slope) slope[j] = gate == 1 ? s * c : s * fmaf(z[j], c, 1.f);
     }
@@ -220,7 +221,7 @@ __global__ void __launch_bounds__(MAXT ? MAXT : kSmallWG) norm_fwd(NormArgs k, i
                 y[j] = now.y.get(j);
                 z[j] = now.z.get(j);
             }
-            gate_values(k.gate, z, v, nullptr);
+            gate_values<DT>(k.gate, z, v, nullptr);
             float rp = 1.f;
             if (k.w_post) {
                 float s[1] = {0.f};
@@ -299,7 +300,7 @@ __global__ void __launch_bounds__(MAXT ? MAXT : kSmallWG) norm_bwd(NormArgs k, i
 #pragma unroll
     for (int j = 0; j < E; ++j) kw[j] *= pre[j];
     cols.weights(k.w_pre, 0.f, pre);
-    gate_values(k.gate, z, v, slope);
+    gate_values<DT>(k.gate, z, v, slope);
     for (long long r0 = b0; r0 < b1; r0 += me.subs) {
         const bool live = r0 + me.sub < b1;
         const long long r = live ? r0 + me.sub : b1 - 1;
@@ -312,7 +313,7 @@ __global__ void __launch_bounds__(MAXT ? MAXT : kSmallWG) norm_bwd(NormArgs k, i
         if (row_gate) {
 #pragma unroll
             for (int j = 0; j < E; ++j) z[j] = now.z.get(j);
-            gate_values(k.gate, z, v, slope);
+            gate_values<DT>(k.gate, z, v, slope);
         }
         const float rp = now.rp, rq = now.rq;
         // n, m and d + rq e of a column
@@ -418,7 +419,7 @@ __global__ void __launch_bounds__(256) norm_bwd_seq(NormArgs k, int parts, float
     const float u = k.part2 ? column_sum<16>(k.part2 + b * parts * k.w, parts, k.w, c, lane, sm) : 0.f;
     if (lane != 0 || c >= k.w) return;
     float z[E] = {(float)pack_load<DT, 1>(k.z, b * k.ldz + c).e[0]}, v[E], slope[E];
-    gate_values(k.gate, z, v, slope);
+    gate_values<DT>(k.gate, z, v, slope);
     const float kw = (k.w_post ? k.w_post[c] : 1.f) * (k.scale ? k.scale[c] : 1.f);
     const float dz[1] = {t * kw * slope[0]};
     pack_store<DT, 1>(k.dz, b * k.w + c, dz);

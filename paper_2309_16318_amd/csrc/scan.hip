@@ -36,10 +36,10 @@ typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
 constexpr unsigned long long kEmpty = ~0ull;  // nothing published yet
 
 // The multiplier s, and the factor q of u, of one element.
-template <int GATE>
+template <int GATE, int DT>
 __device__ __forceinline__ void gate_of(float a, float* s, float* q) {
     if constexpr (GATE == 1) {
-        sigmoid_pair(a, s, q);
+        sigmoid_pair<DT == 0>(a, s, q);
     } else {
         *s = a;
         *q = 1.f;
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(64 * S, 4) scan_tile(ScanArgs k, Board bd, int
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 float s, q;
-                gate_of<GATE>(ra[i].get(v), &s, &q);
+                gate_of<GATE, DT>(ra[i].get(v), &s, &q);
                 const float r = BWD ? s * rg[i].get(v) : q * ru[i].get(v);
                 if (has(i)) {
                     A[v] *= s;
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(64 * S, 4) scan_tile(ScanArgs k, Board bd, int
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 float s, q;
-                gate_of<GATE>(ra[i].get(v), &s, &q);
+                gate_of<GATE, DT>(ra[i].get(v), &s, &q);
                 if constexpr (BWD) {
                     const float lam = h[v] + rg[i].get(v);
                     float d = xp[v];
@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(256) scan_step(const void* a, long long lda, c
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         float s, q;
-        gate_of<GATE>((float)pa.e[v], &s, &q);
+        gate_of<GATE, DT>((float)pa.e[v], &s, &q);
         out[v] = fmaf(s, ps.e[v], q * (float)pu.e[v]);
     }
     pack_store<0, V>(state_out, at, out);

@@ -22,7 +22,7 @@ torch = pytest.importorskip("torch")
 E32 = 2.0 ** -24
 EPS = 1e-6
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
-SIZES = [(1, 1, 1), (1, 2, 8), (2, 3, 5), (3, 70, 16), (1, 5, 100), (2, 7, 128), (1, 3, 511),
+SIZES = [(1, 1, 1), (1, 2, 8), (2, 3, 5), (3, 70, 16), (1, 5, 100), (2, 7, 128), (2, 9, 200), (1, 9, 251), (1, 33, 264), (1, 3, 511),
          (2, 9, 512), (1, 5, 513), (2, 2, 520), (1, 3, 1000), (2, 33, 2048), (1, 3, 4100),
          (1, 3, 8191), (1, 2, 8192), (3, 700, 24), (2, 1500, 64), (70, 3, 12)]
 

@@ -209,6 +209,13 @@ def test_saturated_gates(dev):
     both(a, u, g, x0, gl, None, so.DIRECT, torch.float32)
 
 
+def test_large_logits(dev):
+    """Gates between 1e-37 and 1e-4 off 0 and 1, to float32 precision of their own."""
+    a, u, g, x0, gl = inputs(3, 200, 64, so.SIGMOID, torch.float32, dev)
+    a = torch.sign(a - 1.5) * (8 + 77 * torch.rand_like(a))
+    both(a, u, g, x0, gl, None, so.SIGMOID, torch.float32)
+
+
 def test_growing_products_on_an_empty_state(dev):
     """Multipliers of 1.2 over a chunk and more, inputs that stay in range."""
     a, u, g, x0, gl = inputs(1, 300, 8, so.DIRECT, torch.float32, dev)
