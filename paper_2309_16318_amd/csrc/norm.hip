@@ -455,10 +455,14 @@ int row_threads(int w) {
 }
 
 // Workgroups of the backward pass: enough to fill the chip, few enough that
-// their partial sums are a small part of the traffic.
+// their partial sums are a small part of the traffic.  Two of 256 threads for
+// each CU, or as many threads in smaller ones, two wider ones: 512, 768, 1024 and
+// 1536 of them take, forward and backward of 16384 bfloat16 rows, w 2048 (256
+// threads) 187, 190, 198 and 198 us, w 1024 (128) 120, 112, 103 and 101, w 512
+// (256, four rows at a time) 57, 59, 63 and 68.
 int target_groups(int w) {
     const int g = row_threads(w);
-    return g <= 256 ? 1024 : 512;
+    return g > 64 && g < 256 ? 512 * 256 / g : 512;
 }
 int parts_of(const NormArgs& k) {
     const long long rows = k.z_per_seq ? k.L : (long long)k.B * k.L;
