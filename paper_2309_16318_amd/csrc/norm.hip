@@ -512,7 +512,10 @@ hipError_t launch_norm_fwd(const NormArgs& k, int dtype, hipStream_t st) {
     const bool big = G > 64;
     const int threads = big ? G : kSmallWG, subs = big ? 1 : kSmallWG / G;
     const long long need = ((long long)k.B * k.L + subs - 1) / subs;
-    const long long most = 256 * (2048 / threads);
+    // as many threads as the registers let a CU hold, 1536: of 16384 bfloat16 rows,
+    // w 2048, 512 to 2048 of them a CU take 78, 74 (768), 75 (1024), 71 (1536) and
+    // 75 us, of 8192 float32 rows 56, 53, 52, 52 and 56
+    const long long most = 256LL * 1536 / threads;
     const unsigned grid = (unsigned)(need < most ? need : most);
     return by_kind(dtype, packed(k, dtype), G, [&](auto dt, auto vec, auto bg) {
         norm_fwd<decltype(dt)::value, decltype(vec)::value, decltype(bg)::value>
