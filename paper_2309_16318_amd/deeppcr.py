@@ -562,6 +562,16 @@ def _typed(t, shape, name, dtype, device):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
+def _out(t, shape, name, dtype, device, made):
+    """An output: checked if the caller gave it, else made."""
+    if t is None:
+        t = _torch().empty(shape, dtype=dtype, device=device)
+        made.append(t)
+        return t
+    _typed(t, shape, name, dtype, device)
+    return t
+
+
 def _launch(name, stream, device, args, made):
     """Calls entry point `name` with `args` and the stream, on `device`; what
     the binding allocated (`made`) stays allocated until the stream is past it."""
@@ -608,14 +618,8 @@ def deeppcr_gated_scan_forward(a, u, x0=None, lengths=None, gate: int = GATE_DIR
     _typed(x0, (B, w), "x0", torch.float32, dev)
     _typed(lengths, (B,), "lengths", torch.int32, dev)
     made = []
-    if x is None:
-        x = torch.empty((B, L, w), dtype=a.dtype, device=dev)
-        made.append(x)
-    if x_last is None:
-        x_last = torch.empty((B, w), dtype=torch.float32, device=dev)
-        made.append(x_last)
-    _typed(x, (B, L, w), "x", a.dtype, dev)
-    _typed(x_last, (B, w), "x_last", torch.float32, dev)
+    x = _out(x, (B, L, w), "x", a.dtype, dev, made)
+    x_last = _out(x_last, (B, w), "x_last", torch.float32, dev, made)
     ws, nbytes = _space(workspace, gated_scan_workspace_bytes(B, L, w), dev, made)
     _launch("deeppcr_gated_scan_forward", stream, dev,
             (_addr(a), lda, _addr(u), ldu, _addr(x0), _addr(lengths), _addr(x), _addr(x_last), B, L, w,
@@ -640,18 +644,9 @@ def deeppcr_gated_scan_backward(a, u, x, g, g_last=None, x0=None, lengths=None,
         _typed(t, (B, w), n, torch.float32, dev)
     _typed(lengths, (B,), "lengths", torch.int32, dev)
     made = []
-    if da is None:
-        da = torch.empty((B, L, w), dtype=a.dtype, device=dev)
-        made.append(da)
-    if du is None:
-        du = torch.empty((B, L, w), dtype=a.dtype, device=dev)
-        made.append(du)
-    if dx0 is None:
-        dx0 = torch.empty((B, w), dtype=torch.float32, device=dev)
-        made.append(dx0)
-    for t, n in ((da, "da"), (du, "du")):
-        _typed(t, (B, L, w), n, a.dtype, dev)
-    _typed(dx0, (B, w), "dx0", torch.float32, dev)
+    da = _out(da, (B, L, w), "da", a.dtype, dev, made)
+    du = _out(du, (B, L, w), "du", a.dtype, dev, made)
+    dx0 = _out(dx0, (B, w), "dx0", torch.float32, dev, made)
     ws, nbytes = _space(workspace, gated_scan_workspace_bytes(B, L, w), dev, made)
     _launch("deeppcr_gated_scan_backward", stream, dev,
             (_addr(a), lda, _addr(u), ldu, _addr(x), _addr(x0), _addr(lengths), _addr(g), ldg,
@@ -671,13 +666,12 @@ def deeppcr_gated_scan_step(a, u, state, gate: int = GATE_DIRECT, x=None, state_
     dev = a.device
     lda, ldu = _rows(a, (B, w), "a", a), _rows(u, (B, w), "u", a)
     made = []
-    if x is None:
-        x = torch.empty((B, w), dtype=a.dtype, device=dev)
-        made.append(x)
-    state_out = state if state_out is None else state_out
+    x = _out(x, (B, w), "x", a.dtype, dev, made)
     _typed(state, (B, w), "state", torch.float32, dev)
-    _typed(state_out, (B, w), "state_out", torch.float32, dev)
-    _typed(x, (B, w), "x", a.dtype, dev)
+    if state_out is None:
+        state_out = state
+    else:
+        _typed(state_out, (B, w), "state_out", torch.float32, dev)
     _launch("deeppcr_gated_scan_step", stream, dev,
             (_addr(a), lda, _addr(u), ldu, _addr(state), _addr(state_out), _addr(x), B, w, int(gate),
              dt), made)
@@ -731,21 +725,17 @@ def deeppcr_residual_norm_forward(x, y=None, z=None, w_post=None, scale=None, w_
     z [B, L, w], or [B, w] for one gate per sequence."""
     torch = _torch()
     dt, B, L, w, ldy, ldz, per_seq = _norm_inputs(x, y, z, w_post, scale, w_pre)
-    made = []
-
-    def new(shape, dtype):
-        made.append(torch.empty(shape, dtype=dtype, device=x.device))
-        return made[-1]
-
-    if x_out is None and y is not None:
-        x_out = new((B, L, w), x.dtype)
-    if h is None and w_pre is not None:
-        h = new((B, L, w), x.dtype)
-    _typed(x_out, (B, L, w), "x_out", x.dtype, x.device)
-    _typed(h, (B, L, w), "h", x.dtype, x.device)
-    rpost = new((B, L), torch.float32) if w_post is not None else None
-    rpre = new((B, L), torch.float32) if w_pre is not None else None
-    _launch("deeppcr_residual_norm_forward", stream, x.device,
+    made, dev = [], x.device
+    if x_out is not None or y is not None:
+        x_out = _out(x_out, (B, L, w), "x_out", x.dtype, dev, made)
+    if h is not None or w_pre is not None:
+        h = _out(h, (B, L, w), "h", x.dtype, dev, made)
+    rpost = rpre = None
+    if w_post is not None:
+        rpost = _out(None, (B, L), "rstd_post", torch.float32, dev, made)
+    if w_pre is not None:
+        rpre = _out(None, (B, L), "rstd_pre", torch.float32, dev, made)
+    _launch("deeppcr_residual_norm_forward", stream, dev,
             (_addr(x), _addr(y), ldy, _addr(z), ldz, _addr(w_post), _addr(scale), _addr(w_pre),
              _addr(x_out), _addr(h), _addr(rpost), _addr(rpre), B, L, w, int(gate), per_seq,
              float(eps), dt), made)
@@ -766,13 +756,7 @@ def deeppcr_residual_norm_backward(x, y=None, rstd_post=None, rstd_pre=None, dx_
     made = []
 
     def out(given, like, name, dtype=x.dtype):
-        if like is None:
-            return None
-        if given is None:
-            given = torch.empty(like.shape, dtype=dtype, device=dev)
-            made.append(given)
-        _typed(given, like.shape, name, dtype, dev)
-        return given
+        return None if like is None else _out(given, like.shape, name, dtype, dev, made)
 
     for t, n in ((dx_out, "dx_out"), (dh, "dh")):
         _typed(t, (B, L, w), n, x.dtype, dev)
@@ -804,10 +788,7 @@ def deeppcr_orthogonalize(G, X=None, steps: int = 5, coeffs=(3.4445, -4.7750, 2.
     N, (m, n) = (1 if G.dim() == 2 else G.shape[0]), G.shape[-2:]
     _typed(G, G.shape, "G", G.dtype, G.device)
     made = []
-    if X is None:
-        X = torch.empty_like(G)
-        made.append(X)
-    _typed(X, G.shape, "X", G.dtype, G.device)
+    X = _out(X, G.shape, "X", G.dtype, G.device, made)
     ws, nbytes = _space(workspace, orthogonalize_workspace_bytes(N, m, n), G.device, made)
     ca, cb, cc = (float(c) for c in coeffs)
     _launch("deeppcr_orthogonalize", stream, G.device,
