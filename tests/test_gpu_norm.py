@@ -246,3 +246,9 @@ def test_same_bits_every_time_and_captured(dev, per_seq):
         assert all(torch.equal(s, t) for s, t in zip(want, kept))
         if k == 0:
             assert all(torch.equal(s, t) for s, t in zip(want, first))
+
+
+def test_one_tensor_for_several_inputs(dev):
+    v = inputs(2, 5, 264, no.SILU, False, torch.float32, dev)
+    v["z"], v["dh"], v["scale"] = v["y"], v["dx_out"], v["w_post"]
+    both(v, no.SILU, torch.float32)

@@ -164,3 +164,38 @@ def test_tokens_after_a_prompt(dev):
                 w_pre=p["pre"], gate=deeppcr.GATE_SILU, eps=EPS)
             row, h = f.x_out, f.h
         near(h[:, 0], whole[:, l].double().cpu(), l)
+
+
+def test_tokens_from_a_graph(dev):
+    """One token's norm, step and join captured once and replayed token by token
+    on a running state: the rows of the eager calls."""
+    gen = torch.Generator().manual_seed(9)
+    n, w = 5, 136
+    r = lambda *s: torch.randn(*s, generator=gen).to(dev)
+    pre, post = 1 + 0.3 * r(w), 1 + 0.3 * r(w)
+    x, a, z = (r(n, 1, w).bfloat16() for _ in range(3))
+    state = r(n, w)
+
+    def token(state):
+        h = deeppcr.deeppcr_residual_norm_forward(x, w_pre=pre, eps=EPS).h
+        s = deeppcr.deeppcr_gated_scan_step(a[:, 0], h[:, 0], state, gate=deeppcr.GATE_SIGMOID)
+        f = deeppcr.deeppcr_residual_norm_forward(x, s[:, None], z=z, w_post=post, w_pre=pre,
+                                                  gate=deeppcr.GATE_SILU, eps=EPS)
+        return s, f.x_out, f.h
+
+    token(state.clone())
+    torch.cuda.synchronize()
+    running = state.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = token(running)
+    running.copy_(state)
+    for _ in range(5):
+        for t in (x, a, z):
+            t.copy_(r(n, 1, w))
+        want = token(state)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(running, state)
+        assert all(torch.equal(p, q) for p, q in zip(got, want))

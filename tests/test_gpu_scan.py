@@ -286,7 +286,7 @@ def test_same_bits_every_time(dev):
 
 def test_on_another_stream_and_captured(dev):
     """A captured forward and backward, replayed between eager calls on other
-    data, two graphs on one pool, and calls on a stream of their own."""
+    data, and calls on a stream of their own."""
     a, u, g, x0, gl = inputs(2, 1500, 64, so.SIGMOID, torch.bfloat16, dev)
     x = torch.empty_like(a)
     last, dx0 = torch.empty_like(x0), torch.empty_like(x0)
@@ -321,3 +321,35 @@ def test_on_another_stream_and_captured(dev):
         got = deeppcr.deeppcr_gated_scan_forward(a, u, x0=x0, gate=so.SIGMOID, stream=side)
         side.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(want, got))
+
+
+def test_two_calls_at_once(dev):
+    """Two scans whose tiles wait for each other's, on two streams with a
+    workspace each, in both directions at the same time."""
+    sizes = [(2, 6000, 512), (1, 9000, 260)]
+    data = [inputs(*s, so.SIGMOID, torch.bfloat16, dev, seed=i) for i, s in enumerate(sizes)]
+
+    def forward(d, stream=None):
+        return deeppcr.deeppcr_gated_scan_forward(d[0], d[1], x0=d[3], gate=so.SIGMOID,
+                                                  stream=stream)
+
+    def backward(d, x, stream=None):
+        return deeppcr.deeppcr_gated_scan_backward(d[0], d[1], x, d[2], g_last=d[4], x0=d[3],
+                                                   gate=so.SIGMOID, stream=stream)
+
+    want = [forward(d) for d in data]
+    back = [backward(d, w[0]) for d, w in zip(data, want)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in data]
+    for turn in range(4):
+        first, second = (0, 1) if turn % 2 else (1, 0)
+        got = forward(data[first], streams[0]), backward(data[second], want[second][0], streams[1])
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got[0], want[first]))
+        assert all(torch.equal(p, q) for p, q in zip(got[1], back[second]))
+
+
+def test_one_tensor_for_several_inputs(dev):
+    for L in (3, 700):
+        a, _, _, x0, _ = inputs(2, L, 40, so.SIGMOID, torch.float32, dev)
+        both(a, a, a, x0, x0, None, so.SIGMOID, torch.float32, f"L {L}")
