@@ -268,16 +268,18 @@ struct Product {
     float own, times;   // own D + times P Q, before the shifts
 };
 
-// One tile of BM x BM per workgroup of 2 x 2 waves, in turn over the matrices
+// One tile of BM x BN per workgroup of 2 x 2 waves, in turn over the matrices
 // so that an XCD (workgroups go to the 8 of them in turn) works on few.  Steps of
 // 16 columns leave room for four workgroups on a CU, which hide each other's
 // loads and barriers: 16 matrices of 1024 x 1024 1.35 ms a call, against 1.49 with
 // two workgroups, steps of 32 and the loads two steps ahead in registers.
-template <int BM, int MODE, int OUT>
+template <int BM, int BN, int MODE, int OUT>
 __global__ void __launch_bounds__(256, 4) ortho_product(Product g, int tiles, long long all) {
-    constexpr int BK = 16, MT = BM / 64;
-    constexpr int LD = BM / 64;  // loads of 64 chunks of an operand per wave
-    __shared__ __attribute__((aligned(16))) h16 sm[2][2][BM * 2 * BK];  // buffer, operand
+    constexpr int BK = 16, MT = BM / 64, NT = BN / 64;  // a wave's tiles of 32 x 32
+    // also loads of 64 chunks of an operand per wave
+    constexpr int LD[2] = {MT, NT};
+    __shared__ __attribute__((aligned(16))) h16 sm[2][(BM + BN) * 2 * BK];  // buffer; both operands
+    constexpr int RIGHT = BM * 2 * BK;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long long per = (all + 7) / 8, id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
@@ -285,22 +287,25 @@ __global__ void __launch_bounds__(256, 4) ortho_product(Product g, int tiles, lo
     const long long z = id / tiles;
     int bi, bj;
     if constexpr (MODE == APPLY) {
-        const int nt = g.cols / BM;
+        const int nt = g.cols / BN;
         bi = (int)(id % tiles) / nt;
         bj = (int)(id % tiles) % nt;
     } else {
-        // tiles bi <= bj, column by column
-        const int t = (int)(id % tiles);
+        // tiles on and above the diagonal: of BM columns, column by column, and
+        // of those the BM / BN parts
+        constexpr int H = BM / BN;
+        const int t = (int)(id % tiles) / H;
         bj = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
         while (bj * (bj + 1) / 2 > t) --bj;
         while ((bj + 1) * (bj + 2) / 2 <= t) ++bj;
         bi = t - bj * (bj + 1) / 2;
+        bj = bj * H + (int)(id % tiles) % H;
     }
-    // An operand's tile in a step: BM rows of one panel, or (APPLY's right one)
-    // 16 rows of BM / 16 panels, whose columns are read across.
+    // An operand's tile in a step: BM or BN rows of one panel, or (APPLY's right
+    // one) 16 rows of BN / 16 panels, whose columns are read across.
     constexpr bool ACROSS = MODE == APPLY;
     const h16* src[2] = {g.P.at(z, bi * BM, 0),
-                         ACROSS ? g.Q.at(z, 0, bj * BM) : g.Q.at(z, bj * BM, 0)};
+                         ACROSS ? g.Q.at(z, 0, bj * BN) : g.Q.at(z, bj * BN, 0)};
     const long long ahead[2] = {g.P.rows * 32LL, ACROSS ? 16 * 32LL : g.Q.rows * 32LL};
     // chunk c of a row (2 of hi, 2 of lo) sits at c ^ (row / 4 mod 4): 16 rows
     // that are read together lie in different banks
@@ -310,11 +315,11 @@ __global__ void __launch_bounds__(256, 4) ortho_product(Product g, int tiles, lo
     // that belongs there.
     typedef const __attribute__((address_space(1))) void* Global;
     typedef __attribute__((address_space(3))) void* Lds;
-    long long from[2][LD];
+    long long from[2][MT];
 #pragma unroll
     for (int o = 0; o < 2; ++o)
 #pragma unroll
-        for (int u = 0; u < LD; ++u) {
+        for (int u = 0; u < LD[o]; ++u) {
             const int row = (u * 4 + wave) * 16 + (lane >> 2), c = (lane & 3) ^ ((row >> 2) & 3);
             from[o][u] = ACROSS && o == 1 ? (row >> 4) * (g.Q.rows * 32LL) + (row & 15) * 32 + c * 8
                                           : row * 32 + c * 8;
@@ -323,13 +328,17 @@ __global__ void __launch_bounds__(256, 4) ortho_product(Product g, int tiles, lo
 #pragma unroll
         for (int o = 0; o < 2; ++o)
 #pragma unroll
-            for (int u = 0; u < LD; ++u)
+            for (int u = 0; u < LD[o]; ++u)
                 __builtin_amdgcn_global_load_lds((Global)(src[o] + s * ahead[o] + from[o][u]),
-                                                 (Lds)&sm[buf][o][(u * 4 + wave) * 512], 16, 0, 0);
+                                                 (Lds)&sm[buf][o * RIGHT + (u * 4 + wave) * 512], 16, 0, 0);
     };
-    const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BM / 2);
+    const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
     const int r32 = lane & 31, half = lane >> 5;
-    f32x16 acc[MT][MT] = {};
+    // the wave's first row and column; one that lies below the diagonal has
+    // nothing to do (of square tiles too few do to ask for it)
+    const int r0 = bi * BM + wm, c0 = bj * BN + wn;
+    const bool needed = MODE == APPLY || BM == BN || r0 < c0 + BN / 2;
+    f32x16 acc[MT][NT] = {};
     const int steps = g.K / BK;
     stage(0, 0);
     for (int s = 0; s < steps; ++s) {
@@ -337,38 +346,45 @@ __global__ void __launch_bounds__(256, 4) ortho_product(Product g, int tiles, lo
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         const int buf = s & 1;
-        h16x8 a[MT][2], b[MT][2];
-#pragma unroll
-        for (int t = 0; t < MT; ++t)
+        h16x8 a[MT][2], b[NT][2];
+        if (needed) {
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
-                a[t][p] = *reinterpret_cast<const h16x8*>(&sm[buf][0][chunk(wm + t * 32 + r32, p * 2 + half)]);
-                if constexpr (ACROSS) {
-                    // lane 4 i + j of 16 gives row i, columns 4 j .. 4 j + 3 of a 4 x 16
-                    // block and gets its column 4 i + j
-                    h16x4 v[2];
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const int k = wn + t * 32 + (lane & 16) + half * 8 + u * 4 + ((lane & 15) >> 2);
-                        v[u] = read_across(&sm[buf][1][chunk(k, p * 2 + ((lane & 3) >> 1)) + (lane & 1) * 4]);
+                for (int t = 0; t < MT; ++t)
+                    a[t][p] = *reinterpret_cast<const h16x8*>(&sm[buf][chunk(wm + t * 32 + r32, p * 2 + half)]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    if constexpr (ACROSS) {
+                        // lane 4 i + j of 16 gives row i, columns 4 j .. 4 j + 3 of a 4 x 16
+                        // block and gets its column 4 i + j
+                        h16x4 v[2];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const int k = wn + t * 32 + (lane & 16) + half * 8 + u * 4 + ((lane & 15) >> 2);
+                            v[u] = read_across(&sm[buf][RIGHT + chunk(k, p * 2 + ((lane & 3) >> 1)) + (lane & 1) * 4]);
+                        }
+                        b[t][p] = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                    } else {
+                        b[t][p] = *reinterpret_cast<const h16x8*>(&sm[buf][RIGHT + chunk(wn + t * 32 + r32, p * 2 + half)]);
                     }
-                    b[t][p] = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
-                } else {
-                    b[t][p] = *reinterpret_cast<const h16x8*>(&sm[buf][1][chunk(wn + t * 32 + r32, p * 2 + half)]);
                 }
             }
+        }
         // (the compiler would wait for these loads before any later read of LDS)
         __builtin_amdgcn_sched_barrier(0);
         if (s + 1 < steps) stage(buf ^ 1, s + 1);
         __builtin_amdgcn_sched_barrier(0);
+        if (needed) {
 #pragma unroll
-        for (int p = 0; p < 3; ++p)
+            for (int p = 0; p < 3; ++p)
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+                for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int j = 0; j < MT; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][p == 0], b[j][p == 1],
-                                                                       acc[i][j], 0, 0, 0);
+                    for (int j = 0; j < NT; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][p == 0], b[j][p == 1],
+                                                                           acc[i][j], 0, 0, 0);
+        }
     }
     // a lane holds column r32 of each 32 x 32 tile, rows 8 q + 4 half + 0 .. 3
     // values times kScale, as their parts are
@@ -400,8 +416,9 @@ __global__ void __launch_bounds__(256, 4) ortho_product(Product g, int tiles, lo
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < MT; ++j) {
-            const int row0 = bi * BM + wm + i * 32, col = bj * BM + wn + j * 32 + r32;
+        for (int j = 0; j < NT; ++j) {
+            const int row0 = r0 + i * 32, col0 = c0 + j * 32, col = col0 + r32;
+            if (MODE != APPLY && row0 > col0) continue;
 #pragma unroll
             for (int q = 0; q < 4; q += 2) {
                 h16x4 own_hi[2], own_lo[2];
@@ -445,14 +462,14 @@ __global__ void __launch_bounds__(256, 4) ortho_product(Product g, int tiles, lo
                         hi[u] = x[0];
                         lo[u] = x[1];
                     }
-                    if (OUT < 0 && (MODE == APPLY || bi != bj)) {
+                    if (OUT < 0 && (MODE == APPLY || row0 != col0)) {
                         h16* c = g.C.at(z, row + (lane & 3), col & ~3);
                         *reinterpret_cast<h16x4*>(c) = quad_turn(hi[u]);
                         *reinterpret_cast<h16x4*>(c + kLo) = quad_turn(lo[u]);
                     }
                 }
                 if constexpr (MODE != APPLY) {
-                    // by symmetry the tile across the diagonal
+                    // by symmetry the tile across the diagonal (one on it only here)
                     half_turn(&hi[0], &hi[1]);
                     half_turn(&lo[0], &lo[1]);
                     h16* c = g.C.at(z, col, row0 + 8 * (q + half));
@@ -930,18 +947,26 @@ hipError_t product(const Product& g, int some, hipStream_t st) {
     // Tiles of 128, which read LDS and L2 half as much, where there is more than
     // one for every CU: 8 of 1024 x 1024 694 us against 767 with tiles of 64, 16
     // 1349 and 1436, 64 of 512 x 512 805 and 861, but 4 of 1024 x 1024 585 and 490.
+    // Of symmetric products, which have fewer, 128 x 64: they share the CUs more
+    // evenly, and a wave below the diagonal has nothing to do: 16 of 1024 x 1024
+    // 1319 us against 1362 with whole tiles, 64 of 512 x 512 810 and 833.
     auto tiles_of = [&](int side) {
         const long long ti = g.rows / side, tj = g.cols / side;
         return (int)(MODE == APPLY ? ti * tj : ti * (ti + 1) / 2);
     };
-    const bool large = g.rows % 128 == 0 && g.cols % 128 == 0 && tiles_of(128) * (long long)some > 256;
-    const int BM = large ? 128 : 64, tiles = tiles_of(BM);
-    const long long all = tiles * (long long)some;
-    const unsigned grid = (unsigned)((all + 7) / 8 * 8);
-    if (BM == 128)
-        ortho_product<128, MODE, OUT><<<grid, 256, 0, st>>>(g, tiles, all);
+    auto go = [&](auto bm, auto bn) {
+        constexpr int BM = decltype(bm)::value, BN = decltype(bn)::value;
+        const int tiles = tiles_of(BM) * (BM / BN);
+        const long long all = tiles * (long long)some;
+        const unsigned grid = (unsigned)((all + 7) / 8 * 8);
+        ortho_product<BM, BN, MODE, OUT><<<grid, 256, 0, st>>>(g, tiles, all);
+    };
+    constexpr std::integral_constant<int, 64> n64{};
+    constexpr std::integral_constant<int, 128> n128{};
+    if (g.rows % 128 == 0 && g.cols % 128 == 0 && tiles_of(128) * (long long)some > 256)
+        go(n128, std::integral_constant<int, MODE == APPLY ? 128 : 64>{});
     else
-        ortho_product<64, MODE, OUT><<<grid, 256, 0, st>>>(g, tiles, all);
+        go(n64, n64);
     return hipGetLastError();
 }
 
