@@ -271,14 +271,21 @@ struct Product {
 // One tile of BM x BN per workgroup of 2 x 2 waves, in turn over the matrices
 // so that an XCD (workgroups go to the 8 of them in turn) works on few.  Steps of
 // 16 columns leave room for four workgroups on a CU, which hide each other's
-// loads and barriers: 16 matrices of 1024 x 1024 1.35 ms a call, against 1.49 with
-// two workgroups, steps of 32 and the loads two steps ahead in registers.
+// loads and barriers: 16 matrices of 1024 x 1024 1.35 ms a call in square tiles,
+// against 1.49 with two workgroups, steps of 32 and the loads two steps ahead in
+// registers.
 template <int BM, int BN, int MODE, int OUT>
 __global__ void __launch_bounds__(256, 4) ortho_product(Product g, int tiles, long long all) {
     constexpr int BK = 16, MT = BM / 64, NT = BN / 64;  // a wave's tiles of 32 x 32
     // also loads of 64 chunks of an operand per wave
     constexpr int LD[2] = {MT, NT};
-    __shared__ __attribute__((aligned(16))) h16 sm[2][(BM + BN) * 2 * BK];  // buffer; both operands
+    // Steps under way: one beside the one worked on, where large tiles fill the
+    // chip; three where small ones leave a CU few workgroups to hide their loads: one of
+    // 256 x 256 104 us against 147, two of 1024 x 1024 286 and 445, five of 960 x
+    // 960 441 and 480 (with two of them 114, 304 and 459; of large tiles more than
+    // one gained nothing, 8 of 1024 x 1024 683 us and 683).
+    constexpr int NB = BM == 64 ? 4 : 2;
+    __shared__ __attribute__((aligned(16))) h16 sm[NB][(BM + BN) * 2 * BK];  // buffer; both operands
     constexpr int RIGHT = BM * 2 * BK;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -312,7 +319,9 @@ __global__ void __launch_bounds__(256, 4) ortho_product(Product g, int tiles, lo
     auto chunk = [](int row, int c) { return row * 32 + (c ^ ((row >> 2) & 3)) * 8; };
     // A step's tiles go from memory to LDS without passing registers: a wave's
     // load fills 64 chunks in the lanes' order, so each lane asks for the chunk
-    // that belongs there.
+    // that belongs there.  (Before a read of LDS the compiler waits for all such
+    // loads that it knows of; where later ones are under way it is not told of them.
+    // They write no register, and the loop waits for them itself.)
     typedef const __attribute__((address_space(1))) void* Global;
     typedef __attribute__((address_space(3))) void* Lds;
     long long from[2][MT];
@@ -328,9 +337,18 @@ __global__ void __launch_bounds__(256, 4) ortho_product(Product g, int tiles, lo
 #pragma unroll
         for (int o = 0; o < 2; ++o)
 #pragma unroll
-            for (int u = 0; u < LD[o]; ++u)
-                __builtin_amdgcn_global_load_lds((Global)(src[o] + s * ahead[o] + from[o][u]),
-                                                 (Lds)&sm[buf][o * RIGHT + (u * 4 + wave) * 512], 16, 0, 0);
+            for (int u = 0; u < LD[o]; ++u) {
+                const auto* p = src[o] + s * ahead[o] + from[o][u];
+                const Lds to = (Lds)&sm[buf][o * RIGHT + (u * 4 + wave) * 512];
+                if constexpr (NB == 2) {
+                    __builtin_amdgcn_global_load_lds((Global)p, to, 16, 0, 0);
+                } else {
+                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                                 :
+                                 : "s"((unsigned)(size_t)to), "v"((Global)p)
+                                 : "memory");
+                }
+            }
     };
     const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
     const int r32 = lane & 31, half = lane >> 5;
@@ -340,12 +358,18 @@ __global__ void __launch_bounds__(256, 4) ortho_product(Product g, int tiles, lo
     const bool needed = MODE == APPLY || BM == BN || r0 < c0 + BN / 2;
     f32x16 acc[MT][NT] = {};
     const int steps = g.K / BK;
-    stage(0, 0);
+#pragma unroll
+    for (int s = 0; s < NB - 1; ++s)
+        if (s < steps) stage(s, s);
     for (int s = 0; s < steps; ++s) {
-        // this step's tiles have arrived, and nobody reads the other buffer any more
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        // this step's tiles have arrived (the loads of the NB - 2 steps behind it may
+        // be under way), and nobody reads the buffer before it any more
+        if (NB > 2 && s + NB - 2 < steps)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB - 2) * (MT + NT)) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        const int buf = s & 1;
+        const int buf = s & (NB - 1);
         h16x8 a[MT][2], b[NT][2];
         if (needed) {
 #pragma unroll
@@ -371,9 +395,8 @@ __global__ void __launch_bounds__(256, 4) ortho_product(Product g, int tiles, lo
                 }
             }
         }
-        // (the compiler would wait for these loads before any later read of LDS)
         __builtin_amdgcn_sched_barrier(0);
-        if (s + 1 < steps) stage(buf ^ 1, s + 1);
+        if (s + NB - 1 < steps) stage((s + NB - 1) & (NB - 1), s + NB - 1);
         __builtin_amdgcn_sched_barrier(0);
         if (needed) {
 #pragma unroll
@@ -921,7 +944,7 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
 // ------------------------------------------------------------------- the plan
 // Sides are padded to whole tiles of 64.  (To tiles of 128, from 512 on or above
 // 64: five of 960 x 960 597 us, 26 of 448 x 448 383, 192 of 140 x 140 492, against
-// 476, 291 and 310.)
+// 441, 281 and 233.)
 int padded(int n) { return (n + 63) / 64 * 64; }
 
 struct Plan {
@@ -945,8 +968,9 @@ Plan plan_of(int N, int m, int n) {
 template <int MODE, int OUT>
 hipError_t product(const Product& g, int some, hipStream_t st) {
     // Tiles of 128, which read LDS and L2 half as much, where there is more than
-    // one for every CU: 8 of 1024 x 1024 694 us against 767 with tiles of 64, 16
-    // 1349 and 1436, 64 of 512 x 512 805 and 861, but 4 of 1024 x 1024 585 and 490.
+    // one for every CU: 8 of 1024 x 1024 712 us against 793 with tiles of 64, two of
+    // 2048 x 2048 1214 and 1547, 128 of 256 x 256 361 and 367, but 4 of 1024 x 1024
+    // 554 and 463.
     // Of symmetric products, which have fewer, 128 x 64: they share the CUs more
     // evenly, and a wave below the diagonal has nothing to do: 16 of 1024 x 1024
     // 1319 us against 1362 with whole tiles, 64 of 512 x 512 810 and 833.
