@@ -531,10 +531,11 @@ int deeppcr_residual_norm_backward(const void* x, const void* y, long long ldy, 
  * for every matrix, X = G / (|G|_F + eps), then `steps` times
  *   A = X X^T (X^T X where m > n),   X = ca X + (cb A + cc A A) X
  * (X ca + X (cb A + cc A A)), a polynomial in the singular values that moves
- * them towards one and leaves the singular vectors.  The products run on the
- * float16 matrix cores with float32 accumulation, each value carried by two
- * float16 parts, 22 bits of it (three parts, 24 bits, for sides up to 32).  A zero
- * matrix stays zero; a NaN or infinity stays in its matrix.
+ * them towards one and leaves the singular vectors.  The products are
+ * accumulated in float32.  Where both sides are above 32 they run on float16
+ * matrix cores, each value carried by two float16 parts, 22 bits of it; elsewhere
+ * a value keeps all of its 24 bits.  A zero matrix stays zero; a NaN or infinity
+ * stays in its matrix.
  *   G [N, m, n], X [N, m, n] of type dtype, contiguous; X may be G
  *   steps >= 0; ca, cb, cc finite, |ca| >= 1/16 (the linear term moves small
  *         singular values), and such that the iterates stay moderate:

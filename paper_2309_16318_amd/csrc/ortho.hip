@@ -634,8 +634,9 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
     constexpr int NT = P / 32, PITCH = P + 8;  // a row's 16 bytes more spread the banks
     // Sums of few products have no rounding of their own to hide two parts' in
     // (4 x 4 matrices erred by 1.5 times what float32 products do, 11 x 11 by up
-    // to 1.7): there a value has three parts, all its bits, and a product six terms.
-    constexpr int NP = P == 32 ? 3 : 2;
+    // to 1.7, 4 x 69 by 1.9): there a value has three parts, all its bits, and a
+    // product six terms.
+    constexpr int NP = RT == 1 ? 3 : 2;
     __shared__ __attribute__((aligned(16))) h16 sm[NP][32 * RT * PITCH];
     __shared__ float red[2][NT];
     const int lane = threadIdx.x & 63;
@@ -941,11 +942,135 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
         }
 }
 
+// ------------------------------------------------------------ long matrices
+// A matrix of at most 32 rows (or columns: its transpose), longer than the kernels
+// above hold: products with float32 instructions, because its sums are short (as
+// there) and it has little to compute.  One launch a step and no padding: a
+// workgroup reduces the partial sums of A that the launch before left, forms
+// T = ca I + cb A + cc A A, and takes its columns of X through X' = T X, adding
+// up their part of the next A = X' X'^T.  The iterates are float32 [k, r], in their
+// own range: no shift.  510 matrices of 755 x 5 161 us a call, one of 24 x 330 61, 20 of
+// 32 x 1000 82 (as padded tiles 332, 80 and 126); bound by what a workgroup does before
+// its first column (with 128 columns to each instead of 256, 382, 54 and 88).
+struct Long {
+    const void* G;
+    void* out;
+    float *X, *sums;        // [k, r]; partial sums of A, [parts, 32, 32]
+    const float* before;    // those of the launch before
+    const float4* norms;
+    int nparts, m, n, parts;
+    float ca, cb, cc, eps;
+    bool first, step, last;  // X is still G's; there is a step to do; out instead of X
+};
+
+template <int DT>
+__global__ void __launch_bounds__(256, 3) ortho_long(Long g) {
+    constexpr int PITCH = 33;
+    __shared__ float A[32 * PITCH], T[32 * PITCH], xs[4][32 * PITCH];
+    const int lane = threadIdx.x & 63, r32 = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool tall = g.m > g.n;
+    const int k = tall ? g.n : g.m, r = tall ? g.m : g.n;
+    const long long z = blockIdx.y, base = z * g.m * g.n;
+    float* X = g.X + base;
+    // element 2 u + half of a column is what a lane gives to product u of 16
+    float t[16];
+    if (g.step) {
+        const float* p = g.before + z * g.parts * 1024;
+        for (int e = threadIdx.x; e < 1024; e += 256) {
+            float s = 0.f;
+            for (int i = 0; i < g.parts; ++i) s += p[i * 1024 + e];
+            A[(e >> 5) * PITCH + (e & 31)] = s;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            f32x16 c = {};
+#pragma unroll
+            for (int u = 0; u < 16; ++u) {  // A is symmetric
+                const float a = A[r32 * PITCH + 2 * u + half];
+                c = __builtin_amdgcn_mfma_f32_32x32x2f32(a, a, c, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int row = 8 * (i / 4) + 4 * half + i % 4;
+                T[row * PITCH + r32] = fmaf(g.cc, c[i], g.cb * A[row * PITCH + r32]) +
+                                       (row == r32 ? g.ca : 0.f);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < 16; ++u) t[u] = T[r32 * PITCH + 2 * u + half];
+    }
+    Start s{1.f, 1.f, 0.f};
+    if (g.first) s = start_of(g.norms + z * g.nparts, g.nparts, g.eps);
+    f32x16 sum = {};
+    const int tiles = (r + 31) / 32, t0 = tiles * blockIdx.x / g.parts,
+              t1 = tiles * (blockIdx.x + 1) / g.parts;
+    for (int tile = t0 + wave; tile < t1; tile += 4) {
+        const int col = tile * 32 + r32;
+        const bool live = col < r;
+        auto of_g = [&](int row) { return base + (tall ? (long long)col * k + row : (long long)row * r + col); };
+        float x[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+            const int row = 2 * u + half;
+            x[u] = 0.f;
+            if (live && row < k)
+                x[u] = g.first ? (float)pack_load<DT, 1>(g.G, of_g(row)).e[0] * s.unit * s.inv
+                               : X[(long long)row * r + col];
+        }
+        if (g.step) {
+            f32x16 y = {};
+#pragma unroll
+            for (int u = 0; u < 16; ++u)
+                if (2 * u < k) y = __builtin_amdgcn_mfma_f32_32x32x2f32(t[u], x[u], y, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int row = 8 * (i / 4) + 4 * half + i % 4;
+                const float one[1] = {y[i]};
+                if (live && row < k) {
+                    if (g.last)
+                        pack_store<DT, 1>(g.out, of_g(row), one);
+                    else
+                        X[(long long)row * r + col] = y[i];
+                }
+                xs[wave][r32 * PITCH + row] = y[i];
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < 16; ++u) xs[wave][r32 * PITCH + 2 * u + half] = x[u];
+        }
+        if (!g.last) {
+            wave_sync();
+#pragma unroll
+            for (int u = 0; u < 16; ++u) {
+                const float a = xs[wave][(2 * u + half) * PITCH + r32];
+                sum = __builtin_amdgcn_mfma_f32_32x32x2f32(a, a, sum, 0, 0, 0);
+            }
+            wave_sync();
+        }
+    }
+    if (g.last) return;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        xs[wave][(8 * (i / 4) + 4 * half + i % 4) * PITCH + r32] = sum[i];
+    __syncthreads();
+    for (int e = threadIdx.x; e < 1024; e += 256) {
+        const int at = (e >> 5) * PITCH + (e & 31);
+        g.sums[(z * g.parts + blockIdx.x) * 1024 + e] = (xs[0][at] + xs[1][at]) + (xs[2][at] + xs[3][at]);
+    }
+}
+
 // ------------------------------------------------------------------- the plan
 // Sides are padded to whole tiles of 64.  (To tiles of 128, from 512 on or above
 // 64: five of 960 x 960 597 us, 26 of 448 x 448 383, 192 of 140 x 140 492, against
 // 441, 281 and 233.)
 int padded(int n) { return (n + 63) / 64 * 64; }
+
+// Workgroups that share a matrix's norm.
+int norm_parts(int m, int n) {
+    return (int)std::min<long long>(kParts, ((long long)m * n + 16383) / 16384);
+}
 
 struct Plan {
     int k, r, kp, rp, parts;
@@ -959,7 +1084,7 @@ Plan plan_of(int N, int m, int n) {
     p.kp = padded(p.k);
     p.rp = padded(p.r);
     p.xs = (size_t)p.kp * p.rp * 4;
-    p.parts = (int)std::min<long long>(kParts, ((long long)m * n + 16383) / 16384);
+    p.parts = norm_parts(m, n);
     const size_t each = 3 * p.xs;
     p.some = std::max<long long>(1, std::min<long long>({N, 32768, (long long)((1ull << 30) / each)}));
     return p;
@@ -994,8 +1119,60 @@ hipError_t product(const Product& g, int some, hipStream_t st) {
     return hipGetLastError();
 }
 
-// Sides up to 128.
+// Sides up to 128; at most 32 rows or columns beside longer ones.
 bool small_side(int m, int n) { return std::max(m, n) <= 128; }
+bool long_side(int m, int n) { return std::min(m, n) <= 32; }
+
+// A long matrix's workgroups, two tiles for each wave, and its memory: partial norms,
+// partial sums of A twice, X.  At most 8192 matrices at a time.
+int long_parts(int m, int n) { return std::min(16, (std::max(m, n) + 255) / 256); }
+size_t long_bytes(int m, int n) {
+    return kParts * sizeof(float4) + (2 * (size_t)long_parts(m, n) * 1024 + (size_t)m * n) * 4;
+}
+int long_some(int N) { return std::min(N, 8192); }
+
+template <int DT>
+hipError_t run_long(const void* G, void* X, int N, int m, int n, int steps, float ca, float cb,
+                    float cc, float eps, char* ws, hipStream_t st) {
+    const long long sz = (long long)m * n;
+    const int most = long_some(N), parts = long_parts(m, n), norms = norm_parts(m, n);
+    for (long long at = 0; at < N; at += most) {
+        const int some = (int)std::min<long long>(most, N - at);
+        float4* norm = (float4*)ws;
+        float* sums = (float*)(norm + (size_t)most * kParts);
+        const size_t each = (size_t)most * parts * 1024;
+        Long g{};
+        g.G = (const char*)G + at * sz * sizeof(elem_t<DT>);
+        g.out = (char*)X + at * sz * sizeof(elem_t<DT>);
+        g.X = sums + 2 * each;
+        g.norms = norm;
+        g.nparts = norms;
+        g.m = m;
+        g.n = n;
+        g.parts = parts;
+        g.ca = ca;
+        g.cb = cb;
+        g.cc = cc;
+        g.eps = eps;
+        ortho_norm<DT><<<dim3(norms, some), 256, 0, st>>>(g.G, norm, sz);
+        hipError_t e = hipGetLastError();
+        if (e == hipSuccess && steps == 0) {
+            ortho_scaled<DT><<<dim3(parts, some), 256, 0, st>>>(g.G, g.out, norm, norms, sz, eps);
+            e = hipGetLastError();
+        }
+        for (int s = 0; steps > 0 && s <= steps && e == hipSuccess; ++s) {
+            g.first = s <= 1;
+            g.step = s > 0;
+            g.last = s == steps;
+            g.before = sums + (s & 1 ? 0 : each);
+            g.sums = sums + (s & 1 ? each : 0);
+            ortho_long<DT><<<dim3(parts, some), 256, 0, st>>>(g);
+            e = hipGetLastError();
+        }
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 template <int DT>
 hipError_t run_small(const void* G, void* X, int N, int m, int n, int steps, float ca, float cb,
@@ -1038,6 +1215,8 @@ template <int DT>
 hipError_t run(const void* G, void* X, int N, int m, int n, int steps, float ca, float cb, float cc,
                float eps, char* ws, hipStream_t st) {
     if (small_side(m, n)) return run_small<DT>(G, X, N, m, n, steps, ca, cb, cc, eps, st);
+    if (long_side(m, n))
+        return run_long<DT>(G, X, N, m, n, steps, ca, cb, cc, eps, ws, st);
     const Plan p = plan_of(N, m, n);
     const long long sz = (long long)m * n;
     const Growth growth{fabsf(ca), fabsf(cb), fabsf(cc)};
@@ -1089,6 +1268,7 @@ hipError_t run(const void* G, void* X, int N, int m, int n, int steps, float ca,
 
 size_t ortho_workspace(int N, int m, int n) {
     if (small_side(m, n)) return 256;
+    if (long_side(m, n)) return long_some(N) * long_bytes(m, n);
     const Plan p = plan_of(N, m, n);
     return (size_t)p.some * ((kParts + 16) * sizeof(float4) + 3 * p.xs);
 }

@@ -185,3 +185,35 @@ def test_update_of_the_mlp_gradients(dev):
     dW = deeppcr.deeppcr_mlp_backward(d["W"], d["bias"], d["z0"], res.Z, d["G"])[2]
     check(deeppcr.deeppcr_orthogonalize(dW, eps=0.0), oo.orthogonalize(cpu(dW), eps=0.0),
           torch.float32)
+
+
+@pytest.mark.parametrize("shape", [(3, 5, 700), (2, 700, 5), (4, 32, 129), (2, 5000, 32), (1, 1, 8192),
+                                   (5, 17, 300), (2, 31, 257), (700, 2, 140)], ids=str)
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_long_matrices(dev, shape, kind):
+    G = gradient(*shape, TYPES[kind], dev)
+    for steps in (5, 1, 0):
+        got = deeppcr.deeppcr_orthogonalize(G, steps=steps)
+        check(got, oo.orthogonalize(cpu(G), steps), TYPES[kind], steps)
+        X = G.clone()
+        assert torch.equal(deeppcr.deeppcr_orthogonalize(X, X=X, steps=steps), got)
+
+
+@pytest.mark.parametrize("m, n", [(20, 300), (400, 6)])
+def test_long_matrices_range(dev, m, n):
+    """Far below and above the squares' range, far below eps, zero, not finite."""
+    G = gradient(7, m, n, torch.float32, dev)
+    G[0] *= 1e-37 / 0.02
+    G[1] = G[1] * 50 * 1e37
+    G[2] = 0
+    got = deeppcr.deeppcr_orthogonalize(G, eps=0.0)
+    check(got, oo.orthogonalize(cpu(G), eps=0.0), torch.float32)
+    assert torch.all(got[2] == 0)
+    low = deeppcr.deeppcr_orthogonalize(G * 1e-9)
+    check(low[3:], oo.orthogonalize(cpu(G * 1e-9))[3:], torch.float32)
+    G[3, 0, 0] = float("nan")
+    G[4, m - 1, 2] = float("inf")
+    bad = deeppcr.deeppcr_orthogonalize(G, eps=0.0)
+    keep = [0, 1, 2, 5, 6]
+    assert torch.equal(bad[keep], got[keep])
+    assert torch.isnan(bad[3]).any() and torch.isnan(bad[4]).any()
