@@ -527,7 +527,7 @@ __device__ __forceinline__ float inverse_norm(float top, float sum, float eps, f
 // 4 (lane / 16) + e of column lane % 16, which is how a product leaves a tile and
 // how the next one takes its right operand, and by the symmetry of A and B its
 // left one.  X is turned for the Gram product by lane exchanges.  Three parts to
-// a value, six terms to a product (as P = 32 below).  In the 32 x 32 kernel 1024
+// a value, six terms to a product (as of few rows below).  In the 32 x 32 kernel 1024
 // matrices of 16 x 16 took 12.4 us, 9.0 here (a call).
 template <int DT>
 __global__ void __launch_bounds__(64) ortho_tiny(const void* G, void* out, int m, int n, int steps,
