@@ -154,7 +154,7 @@ __device__ __forceinline__ void gate_values(int gate, const float (&z)[E], float
 #pragma unroll
     for (int j = 0; j < E; ++j) {
         float s, c;
-        sigmoid_pair<DT == 0>(z[j], &s, &c);
+        sigmoid_pair<DT == 0 ? FINE : SHORT>(z[j], &s, &c);
         v[j] = gate == 1 ? s : z[j] * s;
         if (slope) slope[j] = gate == 1 ? s * c : s * fmaf(z[j], c, 1.f);
     }

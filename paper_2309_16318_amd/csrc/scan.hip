@@ -35,11 +35,13 @@ constexpr int kSuper = kBack * S;  // tiles between two published states
 typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
 constexpr unsigned long long kEmpty = ~0ull;  // nothing published yet
 
-// The multiplier s, and the factor q of u, of one element.
+// The multiplier s, and the factor q of u, of one element: to float32 precision
+// of their own whatever the sequences' type, because the states, x_last and dx0
+// that they make are float32.
 template <int GATE, int DT>
 __device__ __forceinline__ void gate_of(float a, float* s, float* q) {
     if constexpr (GATE == 1) {
-        sigmoid_pair<DT == 0>(a, s, q);
+        sigmoid_pair<DT == 1 ? FINE_BF16 : FINE>(a, s, q);
     } else {
         *s = a;
         *q = 1.f;

@@ -353,3 +353,31 @@ def test_one_tensor_for_several_inputs(dev):
     for L in (3, 700):
         a, _, _, x0, _ = inputs(2, L, 40, so.SIGMOID, torch.float32, dev)
         both(a, a, a, x0, x0, None, so.SIGMOID, torch.float32, f"L {L}")
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_states_of_large_logits(dev, kind):
+    """Float32 states of gates between 1e-37 and 3e-4 off 0 and 1, one factor at a
+    time, from sequences of every type: s x, q u and the adjoint's s lam err by the
+    gate's exponential (2^-23), its correction, 1 + t, the reciprocal (2^-23), their
+    product and the last one (2^-24 each), 8 * 2^-24 of the value together at worst."""
+    gen = torch.Generator().manual_seed(3)
+    w, t = 4096, TYPES[kind]
+    a = (8 + 77 * torch.rand(1, 1, w, generator=gen)) * (2 * (torch.rand(1, 1, w, generator=gen) < 0.5) - 1)
+    a, u = a.to(t).to(dev), torch.randn(1, 1, w, generator=gen).to(t).to(dev)
+    x0, none, zero = torch.randn(1, w, generator=gen).to(dev), torch.zeros_like(u), torch.zeros(1, w, device=dev)
+    s, q = so.gates(cpu(a)[:, 0], so.SIGMOID)
+
+    def near(got, factor, value):
+        want = factor * value
+        assert np.all(np.abs(cpu(got) - want) <= 8 * E32 * np.abs(want) + TINY * np.abs(value))
+
+    for v, start, factor, value in ((none, x0, s, cpu(x0)), (u, zero, q, cpu(u)[:, 0])):
+        x, last = deeppcr.deeppcr_gated_scan_forward(a, v, x0=start, gate=so.SIGMOID)
+        near(last, factor, value)
+        state = start.clone()
+        deeppcr.deeppcr_gated_scan_step(a[:, 0], v[:, 0], state, gate=so.SIGMOID)
+        near(state, factor, value)
+        dx0 = deeppcr.deeppcr_gated_scan_backward(a, v, x, none, g_last=x0, x0=start,
+                                                  gate=so.SIGMOID)[2]
+        near(dx0, s, cpu(x0))
