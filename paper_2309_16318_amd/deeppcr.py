@@ -2,7 +2,8 @@
 
 Argument marshalling only: torch tensors provide device memory and the
 current HIP stream; every step of the computation runs in the library's
-kernels.  There is no CPU fallback: if the library is missing, every call
+kernels.  With ``stream`` a call works, and allocates, on that stream instead;
+its inputs have to be ready there (``stream.wait_stream``).  There is no CPU fallback: if the library is missing, every call
 raises.
 """
 from __future__ import annotations
@@ -159,10 +160,40 @@ def _check(t, shape, name):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
-def _stream(stream):
-    torch = _torch()
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+def _stream():
+    return ctypes.c_void_p(_torch().cuda.current_stream().cuda_stream)
+
+
+def _tensors(v):
+    """The tensors of a call's arguments or of what it returns."""
+    if isinstance(v, _torch().Tensor):
+        yield v
+    elif isinstance(v, (tuple, list)):
+        for x in v:
+            yield from _tensors(x)
+    elif hasattr(v, "__dataclass_fields__"):
+        yield from _tensors(tuple(vars(v).values()))
+
+
+def _on(stream, call, *args):
+    """`call` with `stream` as the current stream, so that outputs and workspaces
+    which the binding makes come from that stream's memory: what the caller's own
+    stream has freed may still be read by work on it.  Memory that crosses between
+    the two streams is not given out again before both are past it."""
+    cuda = _torch().cuda
+    given = list(_tensors(args))
+    for t in given:
+        if t.is_cuda and t.device != stream.device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {t.device}")
+    before = cuda.current_stream(stream.device)
+    with cuda.stream(stream):
+        result = call(*args)
+    for t in given:
+        if t.is_cuda:
+            t.record_stream(stream)
+    for t in _tensors(result):
+        t.record_stream(before)
+    return result
 
 
 def _workspace(op, B, L, w, workspace, device):
@@ -176,6 +207,8 @@ def _workspace(op, B, L, w, workspace, device):
 # ------------------------------------------------------------- entry points
 def pcr_solve_block_bidiag(J, r, x=None, transpose: int = 0, workspace=None, stream=None):
     """x with M x = r (transpose=0) or M^T x = r (transpose=1); J [B, L, w, w], r [B, L, w]."""
+    if stream is not None:
+        return _on(stream, pcr_solve_block_bidiag, J, r, x, transpose, workspace)
     torch = _torch()
     B, L, w = r.shape
     _check(J, (B, L, w, w), "J")
@@ -185,7 +218,7 @@ def pcr_solve_block_bidiag(J, r, x=None, transpose: int = 0, workspace=None, str
     _check(x, (B, L, w), "x")
     ws, nbytes = _workspace(OP_PCR, B, L, w, workspace, r.device)
     st = lib().pcr_solve_block_bidiag(_ptr(J), _ptr(r), _ptr(x), B, L, w, int(transpose),
-                                      _ptr(ws), nbytes, _stream(stream))
+                                      _ptr(ws), nbytes, _stream())
     if st != OK:
         raise DeepPCRError(st, "pcr_solve_block_bidiag")
     return x
@@ -194,12 +227,14 @@ def pcr_solve_block_bidiag(J, r, x=None, transpose: int = 0, workspace=None, str
 def pcr_solve_block_bidiag_noalloc(J, r, x, transpose: int = 0, stream=None):
     """The same solve into the caller's x without a workspace: the library
     uses its own fixed scratch array and allocates nothing."""
+    if stream is not None:
+        return _on(stream, pcr_solve_block_bidiag_noalloc, J, r, x, transpose)
     B, L, w = r.shape
     _check(J, (B, L, w, w), "J")
     _check(r, (B, L, w), "r")
     _check(x, (B, L, w), "x")
     st = lib().pcr_solve_block_bidiag_noalloc(_ptr(J), _ptr(r), _ptr(x), B, L, w, int(transpose),
-                                              _stream(stream))
+                                              _stream())
     if st != OK:
         raise DeepPCRError(st, "pcr_solve_block_bidiag_noalloc")
     return x
@@ -209,6 +244,8 @@ def pcr_solve_block_bidiag_chunked(J, r, G: int, x=None, transpose: int = 0, wor
                                    stream=None):
     """The same solve computed over G row chunks (chunk-local PCR keeping each
     chunk's coupling, a pass over the chunk ends, then the apply)."""
+    if stream is not None:
+        return _on(stream, pcr_solve_block_bidiag_chunked, J, r, G, x, transpose, workspace)
     torch = _torch()
     B, L, w = r.shape
     _check(J, (B, L, w, w), "J")
@@ -221,7 +258,7 @@ def pcr_solve_block_bidiag_chunked(J, r, G: int, x=None, transpose: int = 0, wor
         workspace = torch.empty(max(n, 1), dtype=torch.uint8, device=r.device)
     nbytes = workspace.numel() * workspace.element_size()
     st = lib().pcr_solve_block_bidiag_chunked(_ptr(J), _ptr(r), _ptr(x), B, L, w, int(transpose),
-                                              int(G), _ptr(workspace), nbytes, _stream(stream))
+                                              int(G), _ptr(workspace), nbytes, _stream())
     if st != OK:
         raise DeepPCRError(st, "pcr_solve_block_bidiag_chunked")
     return x
@@ -240,6 +277,9 @@ def deeppcr_mlp_forward(W, bias, z0, Z=None, layer: int = TANH_MLP, alpha: float
                         stream=None) -> ForwardResult:
     """Newton + PCR forward pass; raises on EINVAL/EHIP/EWORKSPACE and returns
     ENOCONV / ENONFINITE in ``status``."""
+    if stream is not None:
+        return _on(stream, deeppcr_mlp_forward,
+                   W, bias, z0, Z, layer, alpha, tol, max_iter, Z_init, workspace)
     torch = _torch()
     L, w, _ = W.shape
     B = z0.shape[0]
@@ -257,7 +297,7 @@ def deeppcr_mlp_forward(W, bias, z0, Z=None, layer: int = TANH_MLP, alpha: float
     st = lib().deeppcr_mlp_forward(_ptr(W), _ptr(bias), _ptr(z0), _ptr(Z), B, L, w, int(layer),
                                    float(alpha), float(tol), int(max_iter), _ptr(Z_init),
                                    _ptr(ws), nbytes, ctypes.byref(iters), ctypes.byref(last),
-                                   _stream(stream))
+                                   _stream())
     if st not in (OK, ENOCONV, ENONFINITE):
         raise DeepPCRError(st, "deeppcr_mlp_forward")
     return ForwardResult(Z, iters.value, last.value, st)
@@ -276,6 +316,8 @@ def deeppcr_newton_step(J, F, Z, tol: float = 1e-5, workspace=None,
     """One Newton + PCR iteration for caller-evaluated step values F and
     Jacobians J at the iterate Z (updated in place); ``status`` is OK once
     the update meets ``tol``, ENOCONV before, ENONFINITE on a NaN/Inf."""
+    if stream is not None:
+        return _on(stream, deeppcr_newton_step, J, F, Z, tol, workspace)
     B, L, w = Z.shape
     _check(J, (B, L, w, w), "J")
     _check(F, (B, L, w), "F")
@@ -284,7 +326,7 @@ def deeppcr_newton_step(J, F, Z, tol: float = 1e-5, workspace=None,
     res, mx, mz = ctypes.c_float(0.0), ctypes.c_float(0.0), ctypes.c_float(0.0)
     st = lib().deeppcr_newton_step(_ptr(J), _ptr(F), _ptr(Z), B, L, w, float(tol), _ptr(ws),
                                    nbytes, ctypes.byref(res), ctypes.byref(mx), ctypes.byref(mz),
-                                   _stream(stream))
+                                   _stream())
     if st not in (OK, ENOCONV, ENONFINITE):
         raise DeepPCRError(st, "deeppcr_newton_step")
     return NewtonStepResult(res.value, mx.value, mz.value, st)
@@ -305,6 +347,9 @@ def deeppcr_mlp_forward_residual(W, bias, z0, Z=None, layer: int = TANH_MLP, alp
     """Newton + PCR forward pass stopped by the residual rule (defaults: the
     paper's forward-pass solver settings); raises on EINVAL/EHIP/EWORKSPACE
     and returns ENOCONV / ENONFINITE in ``status``."""
+    if stream is not None:
+        return _on(stream, deeppcr_mlp_forward_residual,
+                   W, bias, z0, Z, layer, alpha, atol, rtol, max_iter, Z_init, workspace)
     torch = _torch()
     L, w, _ = W.shape
     B = z0.shape[0]
@@ -323,7 +368,7 @@ def deeppcr_mlp_forward_residual(W, bias, z0, Z=None, layer: int = TANH_MLP, alp
                                             int(layer), float(alpha), float(atol), float(rtol),
                                             int(max_iter), _ptr(Z_init), _ptr(ws), nbytes,
                                             ctypes.byref(iters), ctypes.byref(res),
-                                            _stream(stream))
+                                            _stream())
     if st not in (OK, ENOCONV, ENONFINITE):
         raise DeepPCRError(st, "deeppcr_mlp_forward_residual")
     return ResidualForwardResult(Z, iters.value, res.value, st)
@@ -332,6 +377,9 @@ def deeppcr_mlp_forward_residual(W, bias, z0, Z=None, layer: int = TANH_MLP, alp
 def deeppcr_mlp_backward(W, bias, z0, Z, G, layer: int = TANH_MLP, alpha: float = 1.0,
                          Lambda=None, dz0=None, dW=None, db=None, workspace=None, stream=None):
     """Transposed-PCR backward pass; returns (Lambda, dz0, dW, db)."""
+    if stream is not None:
+        return _on(stream, deeppcr_mlp_backward,
+                   W, bias, z0, Z, G, layer, alpha, Lambda, dz0, dW, db, workspace)
     torch = _torch()
     L, w, _ = W.shape
     B = z0.shape[0]
@@ -349,7 +397,7 @@ def deeppcr_mlp_backward(W, bias, z0, Z, G, layer: int = TANH_MLP, alpha: float 
     ws, nbytes = _workspace(OP_BWD, B, L, w, workspace, dev)
     st = lib().deeppcr_mlp_backward(_ptr(W), _ptr(bias), _ptr(z0), _ptr(Z), _ptr(G),
                                     _ptr(Lambda), _ptr(dz0), _ptr(dW), _ptr(db), B, L, w,
-                                    int(layer), float(alpha), _ptr(ws), nbytes, _stream(stream))
+                                    int(layer), float(alpha), _ptr(ws), nbytes, _stream())
     if st != OK:
         raise DeepPCRError(st, "deeppcr_mlp_backward")
     return Lambda, dz0, dW, db
@@ -364,6 +412,9 @@ def deeppcr_resnet_forward(W, bias, z0, skip: int, act: int = ACT_RELU, Z=None,
                            stream=None) -> ForwardResult:
     """Newton + PCR forward pass of the collapsed-skip ResNet; raises on
     EINVAL/EHIP/EWORKSPACE and returns ENOCONV / ENONFINITE in ``status``."""
+    if stream is not None:
+        return _on(stream, deeppcr_resnet_forward,
+                   W, bias, z0, skip, act, Z, tol, max_iter, Z_init, workspace)
     torch = _torch()
     L, w, _ = W.shape
     B = z0.shape[0]
@@ -384,7 +435,7 @@ def deeppcr_resnet_forward(W, bias, z0, skip: int, act: int = ACT_RELU, Z=None,
     st = lib().deeppcr_resnet_forward(_ptr(W), _ptr(bias), _ptr(z0), _ptr(Z), B, L, w, int(skip),
                                       int(act), float(tol), int(max_iter), _ptr(Z_init),
                                       _ptr(workspace), nbytes, ctypes.byref(iters),
-                                      ctypes.byref(last), _stream(stream))
+                                      ctypes.byref(last), _stream())
     if st not in (OK, ENOCONV, ENONFINITE):
         raise DeepPCRError(st, "deeppcr_resnet_forward")
     return ForwardResult(Z, iters.value, last.value, st)
@@ -393,6 +444,9 @@ def deeppcr_resnet_forward(W, bias, z0, skip: int, act: int = ACT_RELU, Z=None,
 def deeppcr_resnet_backward(W, z0, Z, G, skip: int, act: int = ACT_RELU, Lambda=None, dz0=None,
                             dW=None, db=None, workspace=None, stream=None):
     """Backward pass of the collapsed-skip ResNet; returns (Lambda, dz0, dW, db)."""
+    if stream is not None:
+        return _on(stream, deeppcr_resnet_backward,
+                   W, z0, Z, G, skip, act, Lambda, dz0, dW, db, workspace)
     torch = _torch()
     L, w, _ = W.shape
     B = z0.shape[0]
@@ -413,7 +467,7 @@ def deeppcr_resnet_backward(W, z0, Z, G, skip: int, act: int = ACT_RELU, Lambda=
     nbytes = workspace.numel() * workspace.element_size()
     st = lib().deeppcr_resnet_backward(_ptr(W), _ptr(z0), _ptr(Z), _ptr(G), _ptr(Lambda),
                                        _ptr(dz0), _ptr(dW), _ptr(db), B, L, w, int(skip),
-                                       int(act), _ptr(workspace), nbytes, _stream(stream))
+                                       int(act), _ptr(workspace), nbytes, _stream())
     if st != OK:
         raise DeepPCRError(st, "deeppcr_resnet_backward")
     return Lambda, dz0, dW, db
@@ -422,6 +476,8 @@ def deeppcr_resnet_backward(W, z0, Z, G, skip: int, act: int = ACT_RELU, Lambda=
 def deeppcr_resnet_seq_forward(W, bias, z0, skip: int, act: int = ACT_RELU, Z=None,
                                launch_per_layer: bool = False, stream=None):
     """Sequential GPU pass of the collapsed-skip ResNet; returns Z."""
+    if stream is not None:
+        return _on(stream, deeppcr_resnet_seq_forward, W, bias, z0, skip, act, Z, launch_per_layer)
     torch = _torch()
     L, w, _ = W.shape
     B = z0.shape[0]
@@ -429,7 +485,7 @@ def deeppcr_resnet_seq_forward(W, bias, z0, skip: int, act: int = ACT_RELU, Z=No
     _check(Z, (B, L, w), "Z")
     st = lib().deeppcr_resnet_seq_forward(_ptr(W), _ptr(bias), _ptr(z0), _ptr(Z), B, L, w,
                                           int(skip), int(act), int(bool(launch_per_layer)),
-                                          _stream(stream))
+                                          _stream())
     if st != OK:
         raise DeepPCRError(st, "deeppcr_resnet_seq_forward")
     return Z
@@ -438,6 +494,9 @@ def deeppcr_resnet_seq_forward(W, bias, z0, skip: int, act: int = ACT_RELU, Z=No
 def deeppcr_resnet_seq_backward(W, z0, Z, G, skip: int, act: int = ACT_RELU, Lambda=None,
                                 dz0=None, launch_per_layer: bool = False, stream=None):
     """Sequential GPU adjoints of the collapsed-skip ResNet; returns (Lambda, dz0)."""
+    if stream is not None:
+        return _on(stream, deeppcr_resnet_seq_backward,
+                   W, z0, Z, G, skip, act, Lambda, dz0, launch_per_layer)
     torch = _torch()
     L, w, _ = W.shape
     B = z0.shape[0]
@@ -446,7 +505,7 @@ def deeppcr_resnet_seq_backward(W, z0, Z, G, skip: int, act: int = ACT_RELU, Lam
     dz0 = torch.empty((B, w), dtype=torch.float32, device=dev) if dz0 is None else dz0
     st = lib().deeppcr_resnet_seq_backward(_ptr(W), _ptr(z0), _ptr(Z), _ptr(G), _ptr(Lambda),
                                            _ptr(dz0), B, L, w, int(skip), int(act),
-                                           int(bool(launch_per_layer)), _stream(stream))
+                                           int(bool(launch_per_layer)), _stream())
     if st != OK:
         raise DeepPCRError(st, "deeppcr_resnet_seq_backward")
     return Lambda, dz0
@@ -455,6 +514,8 @@ def deeppcr_resnet_seq_backward(W, z0, Z, G, skip: int, act: int = ACT_RELU, Lam
 def deeppcr_seq_forward(W, bias, z0, Z=None, layer: int = TANH_MLP, alpha: float = 1.0,
                         launch_per_layer: bool = False, stream=None):
     """Sequential layer-by-layer forward pass on the GPU (the comparison baseline)."""
+    if stream is not None:
+        return _on(stream, deeppcr_seq_forward, W, bias, z0, Z, layer, alpha, launch_per_layer)
     torch = _torch()
     L, w, _ = W.shape
     B = z0.shape[0]
@@ -464,7 +525,7 @@ def deeppcr_seq_forward(W, bias, z0, Z=None, layer: int = TANH_MLP, alpha: float
         Z = torch.empty((B, L, w), dtype=torch.float32, device=z0.device)
     _check(Z, (B, L, w), "Z")
     st = lib().deeppcr_seq_forward(_ptr(W), _ptr(bias), _ptr(z0), _ptr(Z), B, L, w, int(layer),
-                                   float(alpha), int(bool(launch_per_layer)), _stream(stream))
+                                   float(alpha), int(bool(launch_per_layer)), _stream())
     if st != OK:
         raise DeepPCRError(st, "deeppcr_seq_forward")
     return Z
@@ -473,6 +534,9 @@ def deeppcr_seq_forward(W, bias, z0, Z=None, layer: int = TANH_MLP, alpha: float
 def deeppcr_seq_backward(W, bias, z0, Z, G, layer: int = TANH_MLP, alpha: float = 1.0,
                          Lambda=None, dz0=None, launch_per_layer: bool = False, stream=None):
     """Sequential adjoint pass on the GPU; returns (Lambda, dz0)."""
+    if stream is not None:
+        return _on(stream, deeppcr_seq_backward,
+                   W, bias, z0, Z, G, layer, alpha, Lambda, dz0, launch_per_layer)
     torch = _torch()
     L, w, _ = W.shape
     B = z0.shape[0]
@@ -486,7 +550,7 @@ def deeppcr_seq_backward(W, bias, z0, Z, G, layer: int = TANH_MLP, alpha: float 
     _check(dz0, (B, w), "dz0")
     st = lib().deeppcr_seq_backward(_ptr(W), _ptr(bias), _ptr(z0), _ptr(Z), _ptr(G), _ptr(Lambda),
                                     _ptr(dz0), B, L, w, int(layer), float(alpha),
-                                    int(bool(launch_per_layer)), _stream(stream))
+                                    int(bool(launch_per_layer)), _stream())
     if st != OK:
         raise DeepPCRError(st, "deeppcr_seq_backward")
     return Lambda, dz0
@@ -562,40 +626,29 @@ def _typed(t, shape, name, dtype, device):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
-def _out(t, shape, name, dtype, device, made):
+def _out(t, shape, name, dtype, device):
     """An output: checked if the caller gave it, else made."""
     if t is None:
-        t = _torch().empty(shape, dtype=dtype, device=device)
-        made.append(t)
-        return t
+        return _torch().empty(shape, dtype=dtype, device=device)
     _typed(t, shape, name, dtype, device)
     return t
 
 
-def _launch(name, stream, device, args, made):
-    """Calls entry point `name` with `args` and the stream, on `device`; what
-    the binding allocated (`made`) stays allocated until the stream is past it."""
+def _launch(name, device, args):
+    """Calls entry point `name` with `args` and the current stream of `device`, on
+    `device`."""
     cuda = _torch().cuda
     if cuda.current_device() != device.index:
         with cuda.device(device):
-            return _launch(name, stream, device, args, made)
-    if stream is None:
-        st = _entry(name)(*args, _raw_stream()(device.index))
-    else:
-        if stream.device != device:
-            raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
-        st = _entry(name)(*args, stream.cuda_stream)
-        for t in made:
-            t.record_stream(stream)
+            return _launch(name, device, args)
+    st = _entry(name)(*args, _raw_stream()(device.index))
     if st != OK:
         raise DeepPCRError(st, name)
 
 
-def _space(workspace, nbytes, device, made):
+def _space(workspace, nbytes, device):
     if workspace is None:
-        workspace = _torch().empty(max(nbytes, 1), dtype=_torch().uint8, device=device)
-        made.append(workspace)
-        return workspace, nbytes
+        return _torch().empty(max(nbytes, 1), dtype=_torch().uint8, device=device), nbytes
     if workspace.device != device or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {device}")
     return workspace, workspace.numel() * workspace.element_size()
@@ -610,6 +663,9 @@ def deeppcr_gated_scan_forward(a, u, x0=None, lengths=None, gate: int = GATE_DIR
                                x_last=None, workspace=None, stream=None):
     """x_l = s_l x_{l-1} + r_l over [B, L, w] (direct: s = a, r = u; sigmoid:
     s = sigmoid(a), r = (1 - s) u) from x0; returns (x, x_last)."""
+    if stream is not None:
+        return _on(stream, deeppcr_gated_scan_forward,
+                   a, u, x0, lengths, gate, x, x_last, workspace)
     torch = _torch()
     dt = _dtype_code(a, "a")
     B, L, w = a.shape
@@ -617,13 +673,12 @@ def deeppcr_gated_scan_forward(a, u, x0=None, lengths=None, gate: int = GATE_DIR
     lda, ldu = _rows(a, (B, L, w), "a", a), _rows(u, (B, L, w), "u", a)
     _typed(x0, (B, w), "x0", torch.float32, dev)
     _typed(lengths, (B,), "lengths", torch.int32, dev)
-    made = []
-    x = _out(x, (B, L, w), "x", a.dtype, dev, made)
-    x_last = _out(x_last, (B, w), "x_last", torch.float32, dev, made)
-    ws, nbytes = _space(workspace, gated_scan_workspace_bytes(B, L, w), dev, made)
-    _launch("deeppcr_gated_scan_forward", stream, dev,
+    x = _out(x, (B, L, w), "x", a.dtype, dev)
+    x_last = _out(x_last, (B, w), "x_last", torch.float32, dev)
+    ws, nbytes = _space(workspace, gated_scan_workspace_bytes(B, L, w), dev)
+    _launch("deeppcr_gated_scan_forward", dev,
             (_addr(a), lda, _addr(u), ldu, _addr(x0), _addr(lengths), _addr(x), _addr(x_last), B, L, w,
-             int(gate), dt, _addr(ws), nbytes), made)
+             int(gate), dt, _addr(ws), nbytes))
     return x, x_last
 
 
@@ -633,6 +688,9 @@ def deeppcr_gated_scan_backward(a, u, x, g, g_last=None, x0=None, lengths=None,
     """Backward pass of the gated scan from its output x, for g = dLoss/dx and
     g_last = dLoss/dx_last; returns (da, du, dx0).  u may be None for the
     direct gate."""
+    if stream is not None:
+        return _on(stream, deeppcr_gated_scan_backward,
+                   a, u, x, g, g_last, x0, lengths, gate, da, du, dx0, workspace)
     torch = _torch()
     dt = _dtype_code(a, "a")
     B, L, w = a.shape
@@ -643,15 +701,14 @@ def deeppcr_gated_scan_backward(a, u, x, g, g_last=None, x0=None, lengths=None,
     for t, n in ((x0, "x0"), (g_last, "g_last")):
         _typed(t, (B, w), n, torch.float32, dev)
     _typed(lengths, (B,), "lengths", torch.int32, dev)
-    made = []
-    da = _out(da, (B, L, w), "da", a.dtype, dev, made)
-    du = _out(du, (B, L, w), "du", a.dtype, dev, made)
-    dx0 = _out(dx0, (B, w), "dx0", torch.float32, dev, made)
-    ws, nbytes = _space(workspace, gated_scan_workspace_bytes(B, L, w), dev, made)
-    _launch("deeppcr_gated_scan_backward", stream, dev,
+    da = _out(da, (B, L, w), "da", a.dtype, dev)
+    du = _out(du, (B, L, w), "du", a.dtype, dev)
+    dx0 = _out(dx0, (B, w), "dx0", torch.float32, dev)
+    ws, nbytes = _space(workspace, gated_scan_workspace_bytes(B, L, w), dev)
+    _launch("deeppcr_gated_scan_backward", dev,
             (_addr(a), lda, _addr(u), ldu, _addr(x), _addr(x0), _addr(lengths), _addr(g), ldg,
              _addr(g_last), _addr(da), _addr(du), _addr(dx0), B, L, w, int(gate), dt, _addr(ws),
-             nbytes), made)
+             nbytes))
     return da, du, dx0
 
 
@@ -660,21 +717,22 @@ def deeppcr_gated_scan_step(a, u, state, gate: int = GATE_DIRECT, x=None, state_
     """One row [B, w] of the gated scan on running float32 states; writes the
     new states to state_out (default: state, in place) and returns x, the
     states in a's type."""
+    if stream is not None:
+        return _on(stream, deeppcr_gated_scan_step, a, u, state, gate, x, state_out)
     torch = _torch()
     dt = _dtype_code(a, "a")
     B, w = a.shape
     dev = a.device
     lda, ldu = _rows(a, (B, w), "a", a), _rows(u, (B, w), "u", a)
-    made = []
-    x = _out(x, (B, w), "x", a.dtype, dev, made)
+    x = _out(x, (B, w), "x", a.dtype, dev)
     _typed(state, (B, w), "state", torch.float32, dev)
     if state_out is None:
         state_out = state
     else:
         _typed(state_out, (B, w), "state_out", torch.float32, dev)
-    _launch("deeppcr_gated_scan_step", stream, dev,
+    _launch("deeppcr_gated_scan_step", dev,
             (_addr(a), lda, _addr(u), ldu, _addr(state), _addr(state_out), _addr(x), B, w, int(gate),
-             dt), made)
+             dt))
     return x
 
 
@@ -723,22 +781,25 @@ def deeppcr_residual_norm_forward(x, y=None, z=None, w_post=None, scale=None, w_
     """x_out = x + scale act(z) norm(y; w_post), h = norm(x_out; w_pre) over
     [B, L, w]; each piece that is None is left out (without y: h = norm(x)).
     z [B, L, w], or [B, w] for one gate per sequence."""
+    if stream is not None:
+        return _on(stream, deeppcr_residual_norm_forward,
+                   x, y, z, w_post, scale, w_pre, gate, eps, x_out, h)
     torch = _torch()
     dt, B, L, w, ldy, ldz, per_seq = _norm_inputs(x, y, z, w_post, scale, w_pre)
-    made, dev = [], x.device
+    dev = x.device
     if x_out is not None or y is not None:
-        x_out = _out(x_out, (B, L, w), "x_out", x.dtype, dev, made)
+        x_out = _out(x_out, (B, L, w), "x_out", x.dtype, dev)
     if h is not None or w_pre is not None:
-        h = _out(h, (B, L, w), "h", x.dtype, dev, made)
+        h = _out(h, (B, L, w), "h", x.dtype, dev)
     rpost = rpre = None
     if w_post is not None:
-        rpost = _out(None, (B, L), "rstd_post", torch.float32, dev, made)
+        rpost = _out(None, (B, L), "rstd_post", torch.float32, dev)
     if w_pre is not None:
-        rpre = _out(None, (B, L), "rstd_pre", torch.float32, dev, made)
-    _launch("deeppcr_residual_norm_forward", stream, dev,
+        rpre = _out(None, (B, L), "rstd_pre", torch.float32, dev)
+    _launch("deeppcr_residual_norm_forward", dev,
             (_addr(x), _addr(y), ldy, _addr(z), ldz, _addr(w_post), _addr(scale), _addr(w_pre),
              _addr(x_out), _addr(h), _addr(rpost), _addr(rpre), B, L, w, int(gate), per_seq,
-             float(eps), dt), made)
+             float(eps), dt))
     return NormResult(x_out if y is not None else x, h, rpost, rpre)
 
 
@@ -748,26 +809,29 @@ def deeppcr_residual_norm_backward(x, y=None, rstd_post=None, rstd_pre=None, dx_
                                    workspace=None, stream=None) -> NormGrads:
     """Gradients of the residual norm from its inputs, its statistics and
     dx_out, dh; those of pieces that are None are None."""
+    if stream is not None:
+        return _on(stream, deeppcr_residual_norm_backward,
+                   x, y, rstd_post, rstd_pre, dx_out, dh, z, w_post, scale, w_pre, gate, dx, dy,
+                   dz, workspace)
     torch = _torch()
     dt, B, L, w, ldy, ldz, per_seq = _norm_inputs(x, y, z, w_post, scale, w_pre)
     dev = x.device
     for t, n in ((rstd_post, "rstd_post"), (rstd_pre, "rstd_pre")):
         _typed(t, (B, L), n, torch.float32, dev)
-    made = []
 
     def out(given, like, name, dtype=x.dtype):
-        return None if like is None else _out(given, like.shape, name, dtype, dev, made)
+        return None if like is None else _out(given, like.shape, name, dtype, dev)
 
     for t, n in ((dx_out, "dx_out"), (dh, "dh")):
         _typed(t, (B, L, w), n, x.dtype, dev)
     dx, dy, dz = out(dx, x, "dx"), out(dy, y, "dy"), out(dz, z, "dz")
     dpost, dscale, dpre = (out(None, p, "", torch.float32) for p in (w_post, scale, w_pre))
-    ws, nbytes = _space(workspace, residual_norm_workspace_bytes(B, L, w, per_seq), dev, made)
-    _launch("deeppcr_residual_norm_backward", stream, dev,
+    ws, nbytes = _space(workspace, residual_norm_workspace_bytes(B, L, w, per_seq), dev)
+    _launch("deeppcr_residual_norm_backward", dev,
             (_addr(x), _addr(y), ldy, _addr(z), ldz, _addr(w_post), _addr(scale), _addr(w_pre),
              _addr(rstd_post), _addr(rstd_pre), _addr(dx_out), _addr(dh), _addr(dx), _addr(dy),
              _addr(dz), _addr(dpost), _addr(dscale), _addr(dpre), B, L, w, int(gate), per_seq, dt,
-             _addr(ws), nbytes), made)
+             _addr(ws), nbytes))
     return NormGrads(dx, dy, dz, dpost, dscale, dpre)
 
 
@@ -781,19 +845,20 @@ def deeppcr_orthogonalize(G, X=None, steps: int = 5, coeffs=(3.4445, -4.7750, 2.
     """The orthogonalised update of a stack of gradients G [N, m, n] (or one,
     [m, n]): Newton-Schulz steps of the polynomial `coeffs` on G / (|G| + eps);
     X may be G."""
+    if stream is not None:
+        return _on(stream, deeppcr_orthogonalize, G, X, steps, coeffs, eps, workspace)
     torch = _torch()
     dt = _dtype_code(G, "G")
     if not G.is_cuda or G.dim() not in (2, 3):
         raise ValueError("G must be a GPU tensor [N, m, n] or [m, n]")
     N, (m, n) = (1 if G.dim() == 2 else G.shape[0]), G.shape[-2:]
     _typed(G, G.shape, "G", G.dtype, G.device)
-    made = []
-    X = _out(X, G.shape, "X", G.dtype, G.device, made)
-    ws, nbytes = _space(workspace, orthogonalize_workspace_bytes(N, m, n), G.device, made)
+    X = _out(X, G.shape, "X", G.dtype, G.device)
+    ws, nbytes = _space(workspace, orthogonalize_workspace_bytes(N, m, n), G.device)
     ca, cb, cc = (float(c) for c in coeffs)
-    _launch("deeppcr_orthogonalize", stream, G.device,
-            (_addr(G), _addr(X), N, m, n, int(steps), ca, cb, cc, float(eps), dt, _addr(ws), nbytes),
-            made)
+    _launch("deeppcr_orthogonalize", G.device,
+            (_addr(G), _addr(X), N, m, n, int(steps), ca, cb, cc, float(eps), dt, _addr(ws),
+             nbytes))
     return X
 
 

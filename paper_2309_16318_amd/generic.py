@@ -24,6 +24,9 @@ def newton_generic(step_fn, jac_fn, z_start, L: int, tol: float = 1e-5, max_iter
     Start: Z_init, or f_0(z_start) in every row (App. F.2).  Stops once
     max|dZ| < tol * max(1, max|Z|) (tol = 0: exactly max_iter iterations).
     """
+    if stream is not None:  # the step functions' work too
+        return deeppcr._on(stream, newton_generic, step_fn, jac_fn, z_start, L, tol, max_iter,
+                           Z_init, workspace)
     torch = deeppcr._torch()
     B, w = z_start.shape
     if Z_init is not None:
@@ -39,7 +42,7 @@ def newton_generic(step_fn, jac_fn, z_start, L: int, tol: float = 1e-5, max_iter
         Zprev = torch.cat([z_start[:, None, :], Z[:, :-1, :]], dim=1)
         F = step_fn(Zprev).contiguous()
         J = jac_fn(Zprev).contiguous()
-        r = deeppcr.deeppcr_newton_step(J, F, Z, tol=tol, workspace=workspace, stream=stream)
+        r = deeppcr.deeppcr_newton_step(J, F, Z, tol=tol, workspace=workspace)
         last = r.max_update
         # the library's test: OK once converged, ENOCONV to go on
         if r.status != deeppcr.ENOCONV:
