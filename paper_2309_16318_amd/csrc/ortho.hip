@@ -97,7 +97,8 @@ constexpr int kParts = 64;  // most workgroups that share a matrix's norm
 __device__ __forceinline__ float next_unit(float sum) { return sum * 0x1p-80f * 0x1p-80f; }
 
 // Sums of squares of the large, ordinary and small elements of a part of a
-// matrix, so that no square leaves the float32 range.
+// matrix, so that no square and no sum of the at most 2^26 of them leaves the
+// float32 range: 2^26 2^100 of the ordinary ones, 2^26 2^96 of the large ones.
 template <int DT>
 __global__ void __launch_bounds__(256) ortho_norm(const void* G, float4* out, long long sz) {
     __shared__ float sm[3][4];
@@ -110,7 +111,7 @@ __global__ void __launch_bounds__(256) ortho_norm(const void* G, float4* out, lo
     float big = 0.f, mid = 0.f, tiny = 0.f;
     auto add = [&](float g) {
         const float a = fabsf(g);
-        const bool l = a > 0x1p60f, s = a < 0x1p-60f;
+        const bool l = a > 0x1p50f, s = a < 0x1p-60f;
         const float x = l ? g * 0x1p-80f : s ? g * 0x1p80f : g;  // NaN is ordinary
         if (l) big = fmaf(x, x, big);
         if (s) tiny = fmaf(x, x, tiny);

@@ -217,3 +217,19 @@ def test_long_matrices_range(dev, m, n):
     keep = [0, 1, 2, 5, 6]
     assert torch.equal(bad[keep], got[keep])
     assert torch.isnan(bad[3]).any() and torch.isnan(bad[4]).any()
+
+
+@pytest.mark.parametrize("shape", [(129, 129), (20, 300), (70, 400), (1024, 1024)], ids=str)
+def test_squares_that_add_up_beyond_float32(dev, shape):
+    """Elements whose squares are in float32's range and their sum is not, alone, in
+    a single row, and beside larger ones; with no steps too (X = G / |G|)."""
+    scales = [1e13, 1e15, 1e16, 1e17, 3e17, 1e18, 2e18, 1e19, 1e20]
+    G = gradient(len(scales) + 2, *shape, torch.float32, dev) * 50
+    for i, s in enumerate(scales):
+        G[i] *= s
+    G[-2, 0] *= 1e18
+    G[-1] *= 1e17
+    G[-1, :, 1] *= 1e3
+    for steps in (5, 0):
+        got = deeppcr.deeppcr_orthogonalize(G, eps=0.0, steps=steps)
+        check(got, oo.orthogonalize(cpu(G), steps, eps=0.0), torch.float32, steps)
