@@ -233,3 +233,40 @@ def test_squares_that_add_up_beyond_float32(dev, shape):
     for steps in (5, 0):
         got = deeppcr.deeppcr_orthogonalize(G, eps=0.0, steps=steps)
         check(got, oo.orthogonalize(cpu(G), steps, eps=0.0), torch.float32, steps)
+
+
+def float32_products(G, steps=5, coeffs=oo.COEFFS, eps=1e-7):
+    """The update with float32 products."""
+    X = G / (torch.sqrt((G * G).sum((1, 2), keepdim=True)) + eps)
+    tall = X.shape[1] > X.shape[2]
+    if tall:
+        X = X.transpose(1, 2).contiguous()
+    a, b, c = coeffs
+    for _ in range(steps):
+        A = torch.bmm(X, X.transpose(1, 2).contiguous())
+        X = a * X + torch.bmm(b * A + c * torch.bmm(A, A), X)
+    return X.transpose(1, 2) if tall else X
+
+
+# a value has all of its 24 bits up to 32 rows: no more than float32's roundings, and
+# a quarter for chance; two parts round to 2^-23 of a value, twice float32's 2^-24
+PRECISION = [((1000, 4, 4), 1.25), ((300, 11, 11), 1.25), ((200, 16, 16), 1.25), ((100, 24, 24), 1.25),
+             ((100, 4, 69), 1.25), ((60, 32, 32), 1.25), ((40, 128, 17), 1.25), ((40, 5, 755), 1.25),
+             ((20, 32, 2000), 1.25), ((20, 20, 300), 1.25),
+             ((60, 33, 64), 2), ((30, 64, 64), 2), ((20, 100, 100), 2), ((20, 128, 128), 2),
+             ((16, 33, 130), 2), ((16, 33, 1024), 2), ((8, 48, 2048), 2), ((8, 33, 8192), 2),
+             ((8, 4096, 64), 2), ((8, 64, 1024), 2), ((4, 128, 8192), 2), ((2, 256, 8192), 2),
+             ((3, 512, 512), 2), ((300, 128, 512), 2)]
+
+
+@pytest.mark.parametrize("shape, times", PRECISION, ids=str)
+def test_errs_like_float32_products(dev, shape, times):
+    """The error of whole matrices against that of float32 products, over enough
+    entries for chance to average out."""
+    gen = torch.Generator().manual_seed(sum(shape))
+    N, m, n = shape
+    G = (torch.randn(N, m, n, generator=gen) * torch.exp(0.5 * torch.randn(N, 1, n, generator=gen))).to(dev)
+    want = oo.orthogonalize(cpu(G))
+    err = lambda X: np.linalg.norm(cpu(X) - want) / np.linalg.norm(want)
+    got, plain = err(deeppcr.deeppcr_orthogonalize(G)), err(float32_products(G))
+    assert got <= times * plain, (got, plain, got / plain)
