@@ -429,7 +429,7 @@ enum {
  * multipliers, so a direct gate's products over consecutive rows have to stay
  * inside the float32 range (those of multipliers in [-1, 1] do; an underflow
  * to zero is one of theirs).
- * B w <= 2^29 and L <= 2^30; workspace_bytes >=
+ * B w < 2^29 and L <= 2^30; workspace_bytes >=
  * deeppcr_gated_scan_workspace_bytes(B, L, w), which is 0 for invalid sizes.
  */
 size_t deeppcr_gated_scan_workspace_bytes(int B, int L, int w);

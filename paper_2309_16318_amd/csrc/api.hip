@@ -1497,9 +1497,9 @@ bool seq_ok(int B, int L, int w, int dtype) {
     return B >= 1 && L >= 1 && w >= 1 && dtype >= DEEPPCR_F32 && dtype <= DEEPPCR_F16 &&
            (double)B * L * w * 4.0 < 9.0e18;
 }
-// A scan has up to 8 threads per channel, and a launch fewer than 2^32.
+// A scan has up to 8 threads per channel, and a launch has to have fewer than 2^32.
 bool scan_ok(int B, int L, int w, int dtype) {
-    return seq_ok(B, L, w, dtype) && (double)B * w <= 536870912.0 && L <= (1 << 30);
+    return seq_ok(B, L, w, dtype) && (double)B * w < 536870912.0 && L <= (1 << 30);
 }
 
 // A sequence with a row stride starts at any element.

@@ -186,3 +186,14 @@ def test_orthogonalize_rejects_polynomials_that_run_away():
                 (float("nan"), 0, 0), (1, float("inf"), 0)):
         assert _ortho(a=bad[0], b=bad[1], c=bad[2], steps=8, nws=1) == E, bad
     assert _ortho(a=2.0, b=0, c=0, steps=2, nws=1) == W
+
+
+def test_gated_scan_channels_end_below_the_threads_of_a_launch():
+    """With 8 threads to a channel 2^29 channels would be a launch of 2^32 threads."""
+    f = deeppcr.gated_scan_workspace_bytes
+    for B, w in ((1 << 19, 1 << 10), (1 << 29, 1), (1, 1 << 29)):
+        assert f(B, 113, w) == 0
+        for call in (_fwd, _step):
+            assert call(B=B, w=w, lda=w, ldu=w) == E
+        assert _bwd(B=B, w=w, lda=w, ldu=w, ldg=w) == E
+    assert f((1 << 29) - 1, 113, 1) > 0 and f((1 << 19) - 1, 1, 1 << 10) > 0
