@@ -353,9 +353,10 @@ __global__ void __launch_bounds__(256, 4) ortho_product(Product g, int tiles, lo
                 if constexpr (NB == 2) {
                     __builtin_amdgcn_global_load_lds((Global)p, to, 16, 0, 0);
                 } else {
-                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                    // (the address of LDS goes by m0, which the compiler sets)
+                    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                                  :
-                                 : "s"((unsigned)(size_t)to), "v"((Global)p)
+                                 : "v"((Global)p), "{m0}"((unsigned)(size_t)to)
                                  : "memory");
                 }
             }
