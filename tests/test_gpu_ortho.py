@@ -270,3 +270,50 @@ def test_errs_like_float32_products(dev, shape, times):
     err = lambda X: np.linalg.norm(cpu(X) - want) / np.linalg.norm(want)
     got, plain = err(deeppcr.deeppcr_orthogonalize(G)), err(float32_products(G))
     assert got <= times * plain, (got, plain, got / plain)
+
+
+@pytest.mark.parametrize("shape, most", [((7500, 33, 129), 7281), ((9000, 130, 3), 8192)], ids=str)
+def test_parts_of_a_stack(dev, shape, most):
+    """Stacks of which the workspace holds `most` matrices at a time: the second
+    turn uses all of it again."""
+    N, m, n = shape
+    need = deeppcr.orthogonalize_workspace_bytes
+    assert need(most - 1, m, n) < need(most, m, n) == need(most + 1, m, n) == need(N, m, n)
+    G = gradient(N, m, n, torch.float32, dev)
+    got = deeppcr.deeppcr_orthogonalize(G)
+    for part in (slice(0, 4), slice(most - 150, most + 150), slice(N - 4, N)):
+        assert torch.equal(got[part], deeppcr.deeppcr_orthogonalize(G[part].clone()))
+    check(got[most - 2:most + 2], oo.orthogonalize(cpu(G[most - 2:most + 2])), torch.float32)
+    assert torch.equal(deeppcr.deeppcr_orthogonalize(G, X=G), got)
+
+
+@pytest.mark.parametrize("shape", [(2, 33, 200), (3, 300, 40), (1, 64, 129), (2, 48, 1025), (1, 64, 8192),
+                                   (1, 5001, 33), (1, 1100, 2100), (1, 2049, 513)], ids=str)
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_thin_and_large_tiles(dev, shape, kind):
+    """33 to 64 rows or columns beside longer ones (products of four steps), and
+    sides beyond 2048."""
+    G = gradient(*shape, TYPES[kind], dev)
+    for steps in (5, 1, 0) if shape[0] > 1 else (5,):
+        got = deeppcr.deeppcr_orthogonalize(G, steps=steps)
+        check(got, oo.orthogonalize(cpu(G), steps), TYPES[kind], steps)
+
+
+@pytest.mark.parametrize("m, n", [(40, 300), (400, 64)])
+def test_thin_tiles_range(dev, m, n):
+    """Far below and above the squares' range, far below eps, zero, not finite."""
+    G = gradient(7, m, n, torch.float32, dev)
+    G[0] *= 1e-37 / 0.02
+    G[1] = G[1] * 50 * 1e37
+    G[2] = 0
+    got = deeppcr.deeppcr_orthogonalize(G, eps=0.0)
+    check(got, oo.orthogonalize(cpu(G), eps=0.0), torch.float32)
+    assert torch.all(got[2] == 0)
+    low = deeppcr.deeppcr_orthogonalize(G * 1e-9)
+    check(low[3:], oo.orthogonalize(cpu(G * 1e-9))[3:], torch.float32)
+    G[3, 0, 0] = float("nan")
+    G[4, m - 1, 2] = float("inf")
+    bad = deeppcr.deeppcr_orthogonalize(G, eps=0.0)
+    keep = [0, 1, 2, 5, 6]
+    assert torch.equal(bad[keep], got[keep])
+    assert torch.isnan(bad[3]).any() and torch.isnan(bad[4]).any()
