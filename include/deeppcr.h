@@ -532,10 +532,15 @@ int deeppcr_residual_norm_backward(const void* x, const void* y, long long ldy, 
  *   A = X X^T (X^T X where m > n),   X = ca X + (cb A + cc A A) X
  * (X ca + X (cb A + cc A A)), a polynomial in the singular values that moves
  * them towards one and leaves the singular vectors.  The products are
- * accumulated in float32.  Where both sides are above 32 they run on float16
- * matrix cores, each value carried by two float16 parts, 22 bits of it; elsewhere
- * a value keeps all of its 24 bits.  A zero matrix stays zero; a NaN or infinity
- * stays in its matrix.
+ * accumulated in float32.  Unless a side of at most 32 meets one above 128 (float32
+ * products there) they run on float16 matrix cores, each value of X, A and B carried
+ * by parts: by two, to 2^-23 of itself, where both sides are above 32, else by three,
+ * to 2^-24; and no part reaches below 2^-35, where |X|_F starts at one at most (a
+ * matrix with |G|_F below eps is held shifted, and keeps its bits).  As a whole a matrix errs like
+ * one by float32 products, by 0.5 to 1.5 times as much; entries of rows or columns
+ * some 10^-4 and less of the others are off by up to 2^-35 times what the steps
+ * magnify small values by (3.4445^5 = 485 with the usual five), not in proportion
+ * to themselves.  A zero matrix stays zero; a NaN or infinity stays in its matrix.
  *   G [N, m, n], X [N, m, n] of type dtype, contiguous; X may be G
  *   steps >= 0; ca, cb, cc finite, |ca| >= 1/16 (the linear term moves small
  *         singular values), and such that the iterates stay moderate:

@@ -3,10 +3,14 @@
 // more rows than columns is worked on as its transpose, X [k, r] with k <= r.
 //
 // Bound by the matrix cores.  A float32 value is carried by two float16 parts,
-// x 2^10 = hi + lo, 22 bits of it: singular values start at most at 1, and the
-// caller has made sure that no iterate or polynomial passes 15, so 2^10 x stays
-// in range.  A product is hi hi + hi lo + lo hi on the float16 matrix cores
-// with float32 accumulation; lo lo is below 2^-22 of it.  (The float32
+// x 2^10 = hi + lo, to 2^-23 of it and not below 2^-35 (half the spacing of float16's
+// smallest values): singular values start at most at 1, and the caller has made sure
+// that no iterate or polynomial passes 15, so 2^10 x stays in range.  So a matrix as a
+// whole keeps the precision of float32 products, and rows or columns far below the
+// others do not: 150 x 200 with some rows 1e-4, 1e-6 and 1e-8 of the rest has
+// those to 3e-5, 3e-3 and 0.3 of themselves, all by 2e-8 = 2^-35 485, what five steps
+// magnify small values by.  A product is hi hi + hi lo + lo hi on the float16 matrix
+// cores with float32 accumulation; lo lo is below 2^-22 of it.  (The float32
 // instructions have a sixteenth of the float16 ones' rate, against a third.)
 // The iterates stay in these parts between the products.  A and A A are
 // symmetric: their tiles on and above the diagonal are computed and written
@@ -657,8 +661,8 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
     constexpr int NT = P / 32, PITCH = P + 8;  // a row's 16 bytes more spread the banks
     // Sums of few products have no rounding of their own to hide two parts' in
     // (4 x 4 matrices erred by 1.5 times what float32 products do, 11 x 11 by up
-    // to 1.7, 4 x 69 by 1.9): there a value has three parts, all its bits, and a
-    // product six terms.
+    // to 1.7, 4 x 69 by 1.9): there a value has three parts, to 2^-24 of it and not
+    // below 2^-35 either, and a product six terms.
     constexpr int NP = RT == 1 ? 3 : 2;
     __shared__ __attribute__((aligned(16))) h16 sm[NP][32 * RT * PITCH];
     __shared__ float red[2][NT];

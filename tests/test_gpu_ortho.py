@@ -317,3 +317,24 @@ def test_thin_tiles_range(dev, m, n):
     keep = [0, 1, 2, 5, 6]
     assert torch.equal(bad[keep], got[keep])
     assert torch.isnan(bad[3]).any() and torch.isnan(bad[4]).any()
+
+
+@pytest.mark.parametrize("shape", [(16, 16), (100, 120), (30, 100), (150, 200), (40, 300), (20, 400)], ids=str)
+@pytest.mark.parametrize("columns", [False, True])
+def test_rows_far_below_the_others(dev, shape, columns):
+    """Rows or columns 1e-2 to 1e-8 of the rest, each to its own precision or to the
+    parts' floor.  X, A and B are off by up to 2^-35 an entry.  A step's effect on a
+    small row is at most |a| + |X col| (1 + |b| + 2 |c| |A|) of that, with |X| and
+    |A| up to 1.2 and 1.4 the factor 3.5 + 1.2 (1 + 4.8 + 5.7) < 18, and every later
+    step magnifies it by at most 3.45: 18 (3.45^5 - 1) / 2.45 < 2^12 in all."""
+    m, n = shape
+    G = gradient(5, m, n, torch.float32, dev)
+    low = slice(0, n // 8) if columns else slice(0, m // 8)
+    for i, s in enumerate((1e-2, 1e-4, 1e-5, 1e-6, 1e-8)):
+        (G[i].t() if columns else G[i])[low] *= s
+    got, ref = cpu(deeppcr.deeppcr_orthogonalize(G, eps=0.0)), oo.orthogonalize(cpu(G), eps=0.0)
+    if columns:
+        got, ref = got.swapaxes(1, 2), ref.swapaxes(1, 2)
+    e = oo.gain() * (2.0 ** -20 + np.sqrt(max(m, n)) * 2.0 ** -24)
+    top = np.max(np.abs(ref), axis=2, keepdims=True)
+    assert np.all(np.abs(got - ref)[:, low] <= (e * top + 2.0 ** (12 - 35))[:, low])
