@@ -393,7 +393,8 @@ int deeppcr_seq_backward(const float* W, const float* bias, const float* z0, con
  * element, so that it can be a slice of a wider projection's output or a row
  * of a sequence; the others are contiguous.  The conventions above hold for
  * the rest: 16-byte boundaries elsewhere, no allocation,
- * validation before any HIP call, no wait for the GPU, no overlap of an
+ * validation before any HIP call (sizes below 1 are invalid, an empty batch too),
+ * no wait for the GPU, no overlap of an
  * output with another argument but where the text allows it, results that
  * are the same run to run.  Every launch is a kernel, so that each call can
  * sit in a captured graph.
@@ -447,8 +448,10 @@ int deeppcr_gated_scan_forward(const void* a, long long lda, const void* u, long
  *   dx0 = s[0] lam[0]  (g_last for an empty sequence)
  *   a, u, lda, ldu, x0, lengths  as in the forward pass (u may be NULL for
  *                 the direct gate)
- *   x [B, L, w]   the forward pass's output; g [B, L, w] of type dtype, row
- *                 stride ldg
+ *   x [B, L, w]   the forward pass's output, of type dtype: da is formed from these
+ *                 rounded states, so that beside its own rounding it carries theirs
+ *                 (of 16-bit sequences; in float32 ones they are the states)
+ *   g [B, L, w]   of type dtype, row stride ldg
  *   g_last        [B, w] float32, or NULL: zero
  *   da, du        [B, L, w] of type dtype, outputs; zero from row lengths[b] on
  *   dx0           [B, w] float32, output, or NULL; may be g_last

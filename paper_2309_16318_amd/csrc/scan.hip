@@ -5,7 +5,11 @@
 // A x_in + H with A the product of its multipliers and H its end from zero
 // (the diagonal form of the chunk maps P x_in + q of the block solves).  The
 // backward pass is the same recurrence on kap_l = s_l lam_l, the adjoint as
-// it leaves row l: kap_l = s_l kap_{l+1} + s_l g_l, walked from the last row.
+// it leaves row l: kap_l = s_l kap_{l+1} + s_l g_l, walked from the last row.  da
+// is formed from the states as the forward pass stored them, rounded to the
+// sequences' type, which errs by 1.4 times a rounding; forming the float32 states
+// again from a and u would read two sequences more beside the five or six that the
+// pass moves.
 //
 // Bound by memory: every input is read once and every output written once.  A
 // workgroup of S waves takes a tile of S * R rows by 64 packs of V channels;

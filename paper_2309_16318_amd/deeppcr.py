@@ -3,8 +3,10 @@
 Argument marshalling only: torch tensors provide device memory and the
 current HIP stream; every step of the computation runs in the library's
 kernels.  With ``stream`` a call works, and allocates, on that stream instead;
-its inputs have to be ready there (``stream.wait_stream``).  There is no CPU fallback: if the library is missing, every call
-raises.
+its inputs have to be ready there (``stream.wait_stream``).  No call is
+recorded for automatic differentiation: results have no graph, whatever their
+inputs require, and the gradients are the ``_backward`` calls'.  There is no
+CPU fallback: if the library is missing, every call raises.
 """
 from __future__ import annotations
 
@@ -685,9 +687,9 @@ def deeppcr_gated_scan_forward(a, u, x0=None, lengths=None, gate: int = GATE_DIR
 def deeppcr_gated_scan_backward(a, u, x, g, g_last=None, x0=None, lengths=None,
                                 gate: int = GATE_DIRECT, da=None, du=None, dx0=None,
                                 workspace=None, stream=None):
-    """Backward pass of the gated scan from its output x, for g = dLoss/dx and
-    g_last = dLoss/dx_last; returns (da, du, dx0).  u may be None for the
-    direct gate."""
+    """Backward pass of the gated scan from its output x (rounded to its type, as da
+    then is twice), for g = dLoss/dx and g_last = dLoss/dx_last; returns
+    (da, du, dx0).  u may be None for the direct gate."""
     if stream is not None:
         return _on(stream, deeppcr_gated_scan_backward,
                    a, u, x, g, g_last, x0, lengths, gate, da, du, dx0, workspace)
