@@ -381,3 +381,26 @@ def test_states_of_large_logits(dev, kind):
         dx0 = deeppcr.deeppcr_gated_scan_backward(a, v, x, none, g_last=x0, x0=start,
                                                   gate=so.SIGMOID)[2]
         near(dx0, s, cpu(x0))
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("L", [1, 40, 700])
+def test_infinite_logits(dev, kind, L):
+    """A logit of +inf keeps the state, one of -inf takes u, exactly; a NaN stays one."""
+    a, u, g, x0, gl = inputs(2, L, 64, so.SIGMOID, TYPES[kind], dev)
+    keep = torch.rand(a.shape, generator=torch.Generator().manual_seed(L)).to(dev) < 0.7
+    a = torch.where(keep, float("inf"), float("-inf")).to(a.dtype)
+    x, last = deeppcr.deeppcr_gated_scan_forward(a, u, x0=x0, gate=so.SIGMOID)
+    state, want = x0.clone(), []
+    for l in range(L):
+        step = state.clone()
+        y = deeppcr.deeppcr_gated_scan_step(a[:, l], u[:, l], step, gate=so.SIGMOID)
+        state = torch.where(keep[:, l], state, u[:, l].float())
+        assert torch.equal(step, state) and torch.equal(y, state.to(y.dtype))
+        want.append(state.to(x.dtype))
+    assert torch.equal(x, torch.stack(want, 1)) and torch.equal(last, state)
+    da, du, dx0 = deeppcr.deeppcr_gated_scan_backward(a, u, x, g, g_last=gl, x0=x0, gate=so.SIGMOID)
+    assert torch.all(da == 0) and torch.all(du[keep] == 0) and torch.all(torch.isfinite(dx0))
+    a[0, 0, 5] = float("nan")
+    x = deeppcr.deeppcr_gated_scan_forward(a, u, x0=x0, gate=so.SIGMOID)[0]
+    assert torch.isnan(x[0, 0, 5]) and not torch.isnan(x[1]).any() and not torch.isnan(x[0, 0, :5]).any()

@@ -118,3 +118,26 @@ def test_a_stream_of_another_device_is_refused(dev):
     a = torch.rand(1, 4, 8, device=dev)
     with pytest.raises(ValueError):
         deeppcr.deeppcr_gated_scan_forward(a, a, stream=Elsewhere())
+
+
+def test_captured_on_a_stream_beside(dev):
+    """A captured graph that forks to a stream of its own for the call."""
+    a = torch.rand(2, 700, 40, device=dev)
+    u = torch.randn(2, 700, 40, device=dev)
+    side = torch.cuda.Stream()
+    deeppcr.deeppcr_gated_scan_forward(a, u)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        here = torch.cuda.current_stream()
+        side.wait_stream(here)
+        x, last = deeppcr.deeppcr_gated_scan_forward(a, u, stream=side)
+        here.wait_stream(side)
+        y = 2 * x
+    for _ in range(3):
+        u.copy_(torch.randn_like(u))
+        want = deeppcr.deeppcr_gated_scan_forward(a, u)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(x, want[0]) and torch.equal(last, want[1]) and torch.equal(y, 2 * want[0])
