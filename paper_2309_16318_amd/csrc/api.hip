@@ -1520,14 +1520,19 @@ Extent extent(const void* p, double rows, int w, long long ld, int e) {
 bool stride_ok(double rows, int w, long long ld, int e) {
     return ld >= w && rows * (double)ld * e < 9.0e18;
 }
-// Whether an output overlaps an input or another output; outs[i] may be
-// exactly ins[same[i]] (-1: none).
+// Whether an output overlaps an input or another output; outs[i] may be exactly
+// input may_be[i] (-1: none).  Another input that is the same memory may not be an
+// output, but where every element is read by the thread that writes its place
+// (`in_place`) and both lie alike.
 bool clash(std::initializer_list<Extent> ins, std::initializer_list<Extent> outs,
-           std::initializer_list<const void*> same) {
-    auto s = same.begin();
-    for (auto o = outs.begin(); o != outs.end(); ++o, ++s) {
-        for (const Extent& i : ins)
-            if (overlaps(o->p, o->n, i.p, i.n) && !(*s && i.p == *s && o->p == *s)) return true;
+           std::initializer_list<int> may_be, bool in_place = false) {
+    auto m = may_be.begin();
+    for (auto o = outs.begin(); o != outs.end(); ++o, ++m) {
+        for (auto i = ins.begin(); i != ins.end(); ++i) {
+            const bool same = *m >= 0 && i->p == o->p && ins.begin()[*m].p == o->p;
+            const bool meant = i - ins.begin() == *m || (in_place && i->n == o->n);
+            if (overlaps(o->p, o->n, i->p, i->n) && !(same && meant)) return true;
+        }
         for (auto q = o + 1; q != outs.end(); ++q)
             if (overlaps(o->p, o->n, q->p, q->n)) return true;
     }
@@ -1620,7 +1625,7 @@ int deeppcr_gated_scan_forward(const void* a, long long lda, const void* u, long
     if (clash({extent(a, rows, w, lda, e), extent(u, rows, w, ldu, e), {x0, x0 ? state : 0},
                {lengths, lengths ? (size_t)B * 4 : 0}},
               {extent(x, rows, w, w, e), {x_last, x_last ? state : 0}, {workspace, need}},
-              {nullptr, x0, nullptr}))
+              {-1, 2, -1}))
         return DEEPPCR_EINVAL;
     ScanArgs k{};
     k.a = a;
@@ -1668,7 +1673,7 @@ int deeppcr_gated_scan_backward(const void* a, long long lda, const void* u, lon
                {lengths, lengths ? (size_t)B * 4 : 0}},
               {extent(da, rows, w, w, e), extent(du, rows, w, w, e), {dx0, dx0 ? state : 0},
                {workspace, need}},
-              {nullptr, nullptr, g_last, nullptr}))
+              {-1, -1, 5, -1}))
         return DEEPPCR_EINVAL;
     ScanArgs k{};
     k.a = a;
@@ -1707,7 +1712,7 @@ int deeppcr_gated_scan_step(const void* a, long long lda, const void* u, long lo
     if (!stride_ok(B, w, lda, e) || !stride_ok(B, w, ldu, e)) return DEEPPCR_EINVAL;
     const size_t ns = (size_t)B * w * 4;
     if (clash({extent(a, B, w, lda, e), extent(u, B, w, ldu, e), {state, ns}},
-              {{state_out, ns}, extent(x, B, w, w, e)}, {state, nullptr}))
+              {{state_out, ns}, extent(x, B, w, w, e)}, {2, -1}, true))
         return DEEPPCR_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     const double n = (double)B * w;
@@ -1746,7 +1751,7 @@ int deeppcr_residual_norm_forward(const void* x, const void* y, long long ldy, c
                {w_post, nw}, {scale, nw}, {w_pre, nw}},
               {extent(x_out, rows, w, w, e), extent(h, rows, w, w, e), {rstd_post, nr},
                {rstd_pre, nr}},
-              {x, nullptr, nullptr, nullptr}))
+              {0, -1, -1, -1}, true))
         return DEEPPCR_EINVAL;
     NormArgs k{};
     k.x = x;
@@ -1807,7 +1812,7 @@ int deeppcr_residual_norm_backward(const void* x, const void* y, long long ldy, 
                extent(dx_out, rows, w, w, e), extent(dh, rows, w, w, e)},
               {extent(dx, rows, w, w, e), extent(dy, rows, w, w, e), extent(dz, zrows, w, w, e),
                {dw_post, nw}, {dscale, nw}, {dw_pre, nw}, {workspace, need}},
-              {nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr}))
+              {-1, -1, -1, -1, -1, -1, -1}))
         return DEEPPCR_EINVAL;
     NormArgs k{};
     k.x = x;
@@ -1859,7 +1864,7 @@ int deeppcr_orthogonalize(const void* G, void* X, int N, int m, int n, int steps
     const size_t need = ortho_workspace(N, m, n);
     if (workspace_bytes < need) return DEEPPCR_EWORKSPACE;
     const size_t nx = (size_t)N * m * n * elem_size(dtype);
-    if (clash({{G, nx}}, {{X, nx}, {workspace, need}}, {G, nullptr})) return DEEPPCR_EINVAL;
+    if (clash({{G, nx}}, {{X, nx}, {workspace, need}}, {0, -1})) return DEEPPCR_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     const double k = m < n ? m : n, r = m < n ? n : m;
     const hipError_t err =

@@ -197,3 +197,20 @@ def test_gated_scan_channels_end_below_the_threads_of_a_launch():
             assert call(B=B, w=w, lda=w, ldu=w) == E
         assert _bwd(B=B, w=w, lda=w, ldu=w, ldg=w) == E
     assert f((1 << 29) - 1, 113, 1) > 0 and f((1 << 19) - 1, 1, 1 << 10) > 0
+
+
+def test_in_place_means_one_argument():
+    """An output may be the argument that the text names, not another one that is
+    the same memory and laid out, or read, otherwise."""
+    for n in (0, 1):   # the workspace is looked at first: only a large one gets to the overlaps
+        want = E if n else deeppcr.EWORKSPACE
+        nws = BIG if n else 0
+        # dx0 over g_last that is x0 too: x0 is read while dx0 is written
+        assert _bwd(x0=P[6], gl=P[6], dx0=P[6], nws=nws) == want
+        # x_last over x0 that is the gates too
+        assert _fwd(a=P[2], dtype=0, last=P[2], nws=nws) == want
+    # the stream in place, and the block's output the same memory in other rows
+    assert _nfwd(y=P[0], ldy=80, xo=P[0]) == E
+    assert _nfwd(z=P[0], ldz=48, xo=P[0]) == E
+    assert _nfwd(z=P[0], per=1, xo=P[0]) == E
+    assert _step(a=P[2], lda=80, dtype=0, so=P[2]) == E
