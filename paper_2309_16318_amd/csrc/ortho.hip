@@ -286,9 +286,9 @@ __global__ void __launch_bounds__(256, 4) ortho_product(Product g, int tiles, lo
     constexpr int LD[2] = {MT, NT};
     // Steps under way: one beside the one worked on, where large tiles fill the
     // chip; three where small ones leave a CU few workgroups to hide their loads: one of
-    // 256 x 256 104 us against 147, two of 1024 x 1024 286 and 445, five of 960 x
-    // 960 441 and 480 (with two of them 114, 304 and 459; of large tiles more than
-    // one gained nothing, 8 of 1024 x 1024 683 us and 683).
+    // 256 x 256 100 us against 150, two of 1024 x 1024 279 and 451, five of 960 x
+    // 960 492 and 613 (of large tiles more than one gained nothing, 8 of 1024 x 1024
+    // 683 us and 683).
     constexpr int NB = BM == 64 ? 4 : 2;
     // A matrix instruction cuts its 16 products to the bits that the largest of them
     // and the sum leave them (1 + 15 x 0.9 2^-23 gives 1 + 11 x 2^-23), so that a long
@@ -554,8 +554,9 @@ __device__ __forceinline__ float inverse_norm(float top, float sum, float eps, f
 // 4 (lane / 16) + e of column lane % 16, which is how a product leaves a tile and
 // how the next one takes its right operand, and by the symmetry of A and B its
 // left one.  X is turned for the Gram product by lane exchanges.  Three parts to
-// a value, six terms to a product (as of few rows below).  In the 32 x 32 kernel 1024
-// matrices of 16 x 16 took 12.4 us, 9.0 here (a call).
+// a value, six terms to a product (as of few rows below).  1024 matrices of 16 x 16
+// take 6.0 us (in a graph; in the 32 x 32 kernel a call took 12.4 us when it took 9.0
+// here).
 template <int DT>
 __global__ void __launch_bounds__(64) ortho_tiny(const void* G, void* out, int m, int n, int steps,
                                                  float ca, float cb, float cc, float eps,
@@ -989,7 +990,7 @@ __global__ void __launch_bounds__(2 * P, 2) ortho_small(const void* G, void* out
 // workgroup reduces the partial sums of A that the launch before left, forms
 // T = ca I + cb A + cc A A, and takes its columns of X through X' = T X, adding
 // up their part of the next A = X' X'^T.  The iterates are float32 [k, r], in their
-// own range: no shift.  510 matrices of 755 x 5 161 us a call, one of 24 x 330 61, 20 of
+// own range: no shift.  510 matrices of 755 x 5 157 us a call, one of 24 x 330 61, 20 of
 // 32 x 1000 82 (as padded tiles 332, 80 and 126); bound by what a workgroup does before
 // its first column (with 128 columns to each instead of 256, 382, 54 and 88).
 struct Long {
@@ -1102,9 +1103,8 @@ __global__ void __launch_bounds__(256, 3) ortho_long(Long g) {
 }
 
 // ------------------------------------------------------------------- the plan
-// Sides are padded to whole tiles of 64.  (To tiles of 128, from 512 on or above
-// 64: five of 960 x 960 597 us, 26 of 448 x 448 383, 192 of 140 x 140 492, against
-// 441, 281 and 233.)
+// Sides are padded to whole tiles of 64.  (Above 64 to tiles of 128: five of 960 x 960
+// 520 us, 26 of 448 x 448 416, 192 of 140 x 140 431, against 492, 365 and 282.)
 int padded(int n) { return (n + 63) / 64 * 64; }
 
 // Workgroups that share a matrix's norm.
@@ -1133,12 +1133,12 @@ Plan plan_of(int N, int m, int n) {
 template <int MODE, int OUT>
 hipError_t product(const Product& g, int some, hipStream_t st) {
     // Tiles of 128, which read LDS and L2 half as much, where there is more than
-    // one for every CU: 8 of 1024 x 1024 712 us against 793 with tiles of 64, two of
-    // 2048 x 2048 1214 and 1547, 128 of 256 x 256 361 and 367, but 4 of 1024 x 1024
-    // 554 and 463.
+    // one for every CU: 8 of 1024 x 1024 751 us against 794 with tiles of 64, two of
+    // 2048 x 2048 1303 and 1548, 128 of 256 x 256 385 and 404, but 4 of 1024 x 1024
+    // 564 and 471.
     // Of symmetric products, which have fewer, 128 x 64: they share the CUs more
     // evenly, and a wave below the diagonal has nothing to do: 16 of 1024 x 1024
-    // 1319 us against 1362 with whole tiles, 64 of 512 x 512 810 and 833.
+    // 1408 us against 1467 with whole tiles, 64 of 512 x 512 851 and 881.
     auto tiles_of = [&](int side) {
         const long long ti = g.rows / side, tj = g.cols / side;
         return (int)(MODE == APPLY ? ti * tj : ti * (ti + 1) / 2);

@@ -27,7 +27,7 @@ namespace deeppcr {
 namespace {
 
 // Tiles of 64 or 256 rows, packs of 4 and 1 or 4 earlier tiles per wave were
-// measured too: one sequence of 65536 rows of 1024 bfloat16 channels, forward
+// measured too (sigmoid gates short): one sequence of 65536 rows of 1024 bfloat16 channels, forward
 // and backward, 320, 287, 413, 299 and 275 us against 263, 8 of 2048 x 2048 159,
 // 169, 200, 156 and 158 against 158, a prompt of 8192 x 2048 40, 42, 48, 40 and
 // 38 against 39.
